@@ -352,6 +352,128 @@ int fmha_embedding_bwd_sorted(const void* dy, void* workspace, size_t workspace_
                               int32_t hidden, int32_t vocab, int32_t dtype, uint32_t flags, void* dw,
                               void* stream);
 
+/* ==== The attention block of a decoder ==========================================
+ * What follows is beyond the paper, which trains an encoder: the attention of a decoder on the
+ * same unpadded storage, for training and for serving.  A query head h of `heads` shares
+ * the key / value head h / (heads / kv_heads) with its neighbours (grouped heads; kv_heads divides
+ * heads).  Conventions as above: nothing is allocated, everything is enqueued on `stream`,
+ * 16-bit tensors with a token stride each (0 = dense, multiples of 8, at most 2^24), base
+ * pointers 16-byte aligned, sums and softmax statistics in fp32. */
+
+/* ---- Norm and rotation of queries and keys -------------------------------------
+ * Per row t and head, on the head_dim channels x:
+ *   norm (where a gamma is given)  x <- x rstd gamma,  rstd = 1 / sqrt(mean(x^2) + eps)
+ *   rotation of the first rotary_dim channels by the row's position n: the pair (a, b) number i becomes
+ *       (a cos - b sin, a sin + b cos) * magnitude,   angle = n * inv_freq[i]
+ *     FMHA_ROPE_HALF:        pair i = channels (i, i + rotary_dim / 2)
+ *     FMHA_ROPE_INTERLEAVED: pair i = channels (2i, 2i + 1)
+ * in fp32 with one rounding at the end; the angle is formed and reduced in 64 bits, so that far
+ * positions lose nothing.  rotary_dim = 0: no rotation. */
+#define FMHA_ROPE_HALF 0
+#define FMHA_ROPE_INTERLEAVED 1
+typedef struct fmha_rope {
+  int32_t rotary_dim;     /* multiple of 16, at most head_dim */
+  int32_t layout;         /* FMHA_ROPE_* */
+  const double* inv_freq; /* device, [rotary_dim / 2] radians per position */
+  float magnitude;        /* multiplies both cos and sin; 1 = a rotation */
+} fmha_rope_t;
+
+/* The frequencies, on the host: base^(-2i / rotary_dim), made fit for contexts `factor` times as long as the
+ * original_context a model was trained on:
+ *   FMHA_ROPE_PLAIN   as they are
+ *   FMHA_ROPE_LINEAR  divided by factor (positions brought closer)
+ *   FMHA_ROPE_BASE    base * factor^(rotary_dim / (rotary_dim - 2)) in place of base: the slowest pair slows down by
+ *                     factor, the fastest not at all (rotary_dim > 2)
+ *   FMHA_ROPE_PARTS   pairs that turn more than `fast` times over original_context as they are, those that
+ *                     turn fewer than `slow` times divided by factor, a mixture linear in the pair's number between,
+ *                     from pair floor(at(fast)) to ceil(at(slow)), at(r) = rotary_dim ln(original_context / (2 pi r)) / (2 ln base),
+ *                     both kept within [0, rotary_dim - 1]; *magnitude = 0.1 ln(factor) + 1 (1 with factor <= 1)
+ * factor >= 1 (ignored by PLAIN), original_context, fast > slow > 0 for PARTS only.  inv_freq: host, [rotary_dim / 2]
+ * (written); magnitude: host or NULL (written: 1 but for PARTS). */
+#define FMHA_ROPE_PLAIN 0
+#define FMHA_ROPE_LINEAR 1
+#define FMHA_ROPE_BASE 2
+#define FMHA_ROPE_PARTS 3
+int fmha_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, int32_t original_context,
+                          double fast, double slow, double* inv_freq, float* magnitude);
+
+typedef struct fmha_qk_params {
+  int32_t rows;       /* rows the buffers hold */
+  int32_t q_heads;    /* >= 0; 0: no queries (their pointers are not looked at) */
+  int32_t k_heads;    /* >= 0, likewise */
+  int32_t head_dim;   /* multiple of 16, at most 256 */
+  int32_t dtype;      /* fmha_dtype_t */
+  float eps;          /* >= 0 */
+  int64_t q_stride, k_stride;         /* elements between rows, 0 = dense */
+  int64_t q_out_stride, k_out_stride; /* of the outputs (backward: of their gradients) */
+  int64_t dq_stride, dk_stride;       /* backward only */
+  const float* gamma_q; /* device, [head_dim], 16-byte aligned, or NULL: no norm of the queries */
+  const float* gamma_k; /* likewise for the keys */
+  /* Positions: positions[t] where that is given (any int32, negative ones too), else the place of row t in its sequence
+   * by cu_seqlens.  One of the two is needed for a rotation. */
+  const int32_t* positions;  /* device, [rows], or NULL */
+  const int32_t* cu_seqlens; /* device, [batch + 1], or NULL */
+  int32_t batch;             /* sequences in cu_seqlens, >= 1 where that is given */
+  const int32_t* n_rows;     /* optional device int32: rows present.  NULL: cu_seqlens[batch], or `rows` without
+                                cu_seqlens.  Rows beyond are neither read nor written. */
+  fmha_rope_t rope;
+} fmha_qk_params_t;
+
+/* Forward, one launch.  q [rows, q_heads, head_dim], k [rows, k_heads, head_dim] (read), q_out, k_out likewise
+ * (written).  An output may be its own input (same pointer and stride); otherwise they must not overlap. */
+int fmha_qk_norm_rope_fwd(const fmha_qk_params_t* p, const void* q, const void* k, void* q_out, void* k_out, void* stream);
+
+/* Bytes of device workspace of the backward (sums for gamma by workgroup); 0 on invalid sizes. */
+size_t fmha_qk_norm_rope_bwd_workspace_size(int32_t rows, int32_t q_heads, int32_t k_heads, int32_t head_dim);
+
+/* Backward: dq_out, dk_out are the gradients of q_out, k_out; q, k the forward's INPUTS (not needed, and may be NULL,
+ * where there is no gamma).  With g the turned-back gradient and xh = x rstd:
+ *   dx = rstd (g gamma - xh mean(g gamma xh)),  dgamma = sum over rows and heads of g xh   (dx = g without a gamma)
+ * dq, dk are written (each may be its own dq_out / dk_out); dgamma_q, dgamma_k (fp32, [head_dim]) are written where
+ * the gamma is given.  Two launches with a gamma, one without; the sums have a fixed order. */
+int fmha_qk_norm_rope_bwd(const fmha_qk_params_t* p, const void* dq_out, const void* dk_out, const void* q, const void* k,
+                          void* dq, void* dk, float* dgamma_q, float* dgamma_k, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* ---- A paged cache of keys and values ---------------------------------------------
+ * Page g holds page_size tokens of all heads: element (head h, place s, channel c) at
+ *   k[g * page_stride + (h * page_size + s) * head_dim + c],   v likewise
+ * (head by head, so that what one head's attention reads of a page is one run).  Token n of sequence b is in page
+ * block_table[b * max_pages + n / page_size], place n % page_size.  Page numbers outside [0, num_pages) name no page:
+ * what would be written there is dropped, and keys there are not attended; so are tokens at and beyond max_pages * page_size. */
+typedef struct fmha_cache {
+  int32_t batch;     /* sequences */
+  int32_t kv_heads;
+  int32_t head_dim;
+  int32_t dtype;     /* fmha_dtype_t */
+  int32_t page_size; /* a power of two, at most 65536 */
+  int32_t num_pages; /* pages that k and v hold */
+  int32_t max_pages; /* columns of block_table */
+  int64_t page_stride;        /* elements between pages, 0 = dense; a multiple of 8 */
+  const int32_t* block_table; /* device, [batch, max_pages] */
+  const int32_t* seqlens;     /* device, [batch]: tokens of each sequence, the newest among them */
+} fmha_cache_t;
+
+typedef struct fmha_append_params {
+  int32_t rows;    /* rows of q, k, v */
+  int32_t q_heads; /* 0: no queries in this call */
+  float eps;
+  int64_t q_stride, k_stride, v_stride, q_out_stride; /* 0 = dense */
+  const float* gamma_q;      /* as in fmha_qk_params_t */
+  const float* gamma_k;
+  const int32_t* cu_seqlens; /* device, [batch + 1]: rows of each sequence; NULL: one row each (rows = batch) */
+  fmha_rope_t rope;
+} fmha_append_params_t;
+
+/* The newest tokens of every sequence go into the cache, one launch.  Rows cu_seqlens[b] .. cu_seqlens[b+1]-1 are the LAST
+ * tokens of sequence b: row cu_seqlens[b+1]-1 has position seqlens[b]-1.  k [rows, kv_heads, head_dim] is normed and rotated
+ * by its position (fmha_qk_norm_rope_fwd) on its way to k_cache, v copied to v_cache; q [rows, q_heads, head_dim] is treated
+ * like k and written to q_out (which may be q).  head_dim: multiple of 16, at most 256.  A row with a negative position
+ * goes to no page.  Rows beyond cu_seqlens[batch] are neither read nor written.  Two rows that the tables send to the same place:
+ * one of them stays, or parts of both. */
+int fmha_cache_append(const fmha_cache_t* c, const fmha_append_params_t* p, const void* q, const void* k, const void* v,
+                      void* q_out, void* k_cache, void* v_cache, void* stream);
+
 /* Number of 128-row tiles the schedule holds at most for this shape (host
  * arithmetic), and a device-to-host-free way for tests to locate the tile list
  * inside the workspace: the list starts at byte offset *list_offset and holds

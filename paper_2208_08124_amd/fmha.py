@@ -22,6 +22,8 @@ FMHA_FLAG_BWD_ONLY_DKV = 4
 FMHA_EMB_ZERO_FIRST = 1
 FMHA_EMB_PLAIN_SPLIT = 2
 FMHA_EMB_NO_DIE_SPLIT = 4
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 
 EXPORTS = ("fmha_varlen_workspace_size", "fmha_varlen_fwd", "fmha_varlen_bwd",
            "fmha_varlen_fwd_static", "fmha_varlen_static_scratch_bytes",
@@ -30,6 +32,8 @@ EXPORTS = ("fmha_varlen_workspace_size", "fmha_varlen_fwd", "fmha_varlen_bwd",
            "fmha_dropout_add_ln_fwd", "fmha_dropout_add_ln_bwd", "fmha_dropout_add_ln_bwd_workspace_size",
            "fmha_embedding_bwd", "fmha_embedding_sort_workspace_size", "fmha_embedding_sort",
            "fmha_embedding_bwd_sorted",
+           "fmha_rope_frequencies", "fmha_qk_norm_rope_fwd", "fmha_qk_norm_rope_bwd",
+           "fmha_qk_norm_rope_bwd_workspace_size", "fmha_cache_append",
            "fmha_varlen_schedule_info", "fmha_last_error")
 
 
@@ -58,6 +62,39 @@ class LnParams(ctypes.Structure):
     """Mirror of fmha_ln_params_t."""
     _fields_ = [("rows", ctypes.c_int32), ("hidden", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("n_rows", ctypes.c_void_p), ("dropout", Dropout)]
+
+
+class RopeArgs(ctypes.Structure):
+    """Mirror of fmha_rope_t."""
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("inv_freq", ctypes.c_void_p),
+                ("magnitude", ctypes.c_float)]
+
+
+class QkParams(ctypes.Structure):
+    """Mirror of fmha_qk_params_t."""
+    _fields_ = [("rows", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("k_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64),
+                ("k_out_stride", ctypes.c_int64), ("dq_stride", ctypes.c_int64), ("dk_stride", ctypes.c_int64),
+                ("gamma_q", ctypes.c_void_p), ("gamma_k", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("cu_seqlens", ctypes.c_void_p), ("batch", ctypes.c_int32), ("n_rows", ctypes.c_void_p),
+                ("rope", RopeArgs)]
+
+
+class Cache(ctypes.Structure):
+    """Mirror of fmha_cache_t."""
+    _fields_ = [("batch", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("page_stride", ctypes.c_int64), ("block_table", ctypes.c_void_p),
+                ("seqlens", ctypes.c_void_p)]
+
+
+class AppendParams(ctypes.Structure):
+    """Mirror of fmha_append_params_t."""
+    _fields_ = [("rows", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("q_out_stride", ctypes.c_int64), ("gamma_q", ctypes.c_void_p), ("gamma_k", ctypes.c_void_p),
+                ("cu_seqlens", ctypes.c_void_p), ("rope", RopeArgs)]
 
 
 class FmhaError(RuntimeError):
@@ -122,6 +159,18 @@ def lib():
         L.fmha_embedding_sort.restype = ctypes.c_int
         L.fmha_embedding_bwd_sorted.argtypes = [vp, vp, ctypes.c_size_t, i32, i32, i32, i32, ctypes.c_uint32, vp, vp]
         L.fmha_embedding_bwd_sorted.restype = ctypes.c_int
+        qp, cp = ctypes.POINTER(QkParams), ctypes.POINTER(Cache)
+        f64 = ctypes.c_double
+        L.fmha_rope_frequencies.argtypes = [i32, f64, i32, f64, i32, f64, f64, vp, ctypes.POINTER(ctypes.c_float)]
+        L.fmha_rope_frequencies.restype = ctypes.c_int
+        L.fmha_qk_norm_rope_fwd.argtypes = [qp] + [vp] * 5
+        L.fmha_qk_norm_rope_fwd.restype = ctypes.c_int
+        L.fmha_qk_norm_rope_bwd_workspace_size.argtypes = [i32] * 4
+        L.fmha_qk_norm_rope_bwd_workspace_size.restype = ctypes.c_size_t
+        L.fmha_qk_norm_rope_bwd.argtypes = [qp] + [vp] * 9 + [ctypes.c_size_t, vp]
+        L.fmha_qk_norm_rope_bwd.restype = ctypes.c_int
+        L.fmha_cache_append.argtypes = [cp, ctypes.POINTER(AppendParams)] + [vp] * 7
+        L.fmha_cache_append.restype = ctypes.c_int
         L.fmha_varlen_schedule_info.argtypes = [ctypes.c_int32] * 3 + [ctypes.POINTER(ctypes.c_size_t)] * 2
         L.fmha_varlen_schedule_info.restype = ctypes.c_int32
         L.fmha_last_error.restype = ctypes.c_char_p
@@ -415,3 +464,158 @@ def fmha_embedding_bwd(dy, indices, dw, *, padding_idx=-1, n_rows=None, zero_fir
     _check(lib().fmha_embedding_bwd(dy.data_ptr(), indices.data_ptr(), None if n_rows is None else n_rows.data_ptr(),
                                     dy.shape[0], dy.shape[1], dw.shape[0], int(padding_idx), _dtype_code(dy), flags,
                                     dw.data_ptr(), _stream()))
+
+
+def fmha_rope_frequencies(rotary_dim, base=10000.0, scaling="plain", factor=1.0, original_context=0, fast=32.0,
+                          slow=1.0):
+    """(inv_freq, magnitude): the frequencies of the rotary_dim / 2 pairs as a CPU float64 tensor, made fit for
+    contexts `factor` times as long by "linear", "base" or "parts" (see the header)."""
+    out = torch.empty(max(int(rotary_dim) // 2, 0), dtype=torch.float64)
+    m = ctypes.c_float(1.0)
+    if scaling not in ROPE_SCALINGS:
+        raise FmhaError(FMHA_ERR_INVALID_ARG, f"scaling {scaling!r} is not one of {sorted(ROPE_SCALINGS)}")
+    _check(lib().fmha_rope_frequencies(int(rotary_dim), float(base), ROPE_SCALINGS[scaling], float(factor),
+                                       int(original_context), float(fast), float(slow), out.data_ptr(), ctypes.byref(m)))
+    return out, float(m.value)
+
+
+def _rope(rope):
+    """(inv_freq float64 device tensor, "half" | "interleaved", magnitude) or None -> fmha_rope_t"""
+    if rope is None:
+        return RopeArgs(0, 0, None, 1.0)
+    inv_freq, layout, magnitude = rope
+    assert inv_freq.dtype == torch.float64 and inv_freq.is_cuda and inv_freq.is_contiguous()
+    if layout not in ROPE_LAYOUTS:
+        raise FmhaError(FMHA_ERR_INVALID_ARG, f"layout {layout!r} is not one of {sorted(ROPE_LAYOUTS)}")
+    return RopeArgs(2 * inv_freq.numel(), ROPE_LAYOUTS[layout], inv_freq.data_ptr(), float(magnitude))
+
+
+def _i32_ptr(t, at_least=None):
+    if t is None:
+        return None
+    assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()
+    assert at_least is None or t.numel() >= at_least
+    return t.data_ptr()
+
+
+def _gamma_ptr(g, dim):
+    if g is None:
+        return None
+    assert g.dtype == torch.float32 and g.is_cuda and g.is_contiguous() and g.numel() == dim
+    return g.data_ptr()
+
+
+def _opt_ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _same_kind(like, *tensors):
+    for t in tensors:
+        assert t is None or (t.dtype == like.dtype and t.is_cuda and t.shape == like.shape)
+
+
+def _qk_params(q, k, rope, gamma_q, gamma_k, eps, positions, cu_seqlens, n_rows):
+    x = q if q is not None else k
+    p = QkParams()
+    p.rows, _, p.head_dim = x.shape
+    if q is not None and k is not None:
+        assert q.shape[0] == k.shape[0] and q.shape[2] == k.shape[2] and q.dtype == k.dtype
+    p.q_heads = 0 if q is None else q.shape[1]
+    p.k_heads = 0 if k is None else k.shape[1]
+    p.dtype = _dtype_code(x)
+    p.eps = float(eps)
+    p.gamma_q, p.gamma_k = _gamma_ptr(gamma_q, p.head_dim), _gamma_ptr(gamma_k, p.head_dim)
+    p.positions = _i32_ptr(positions, p.rows)
+    p.cu_seqlens = _i32_ptr(cu_seqlens)
+    p.batch = 0 if cu_seqlens is None else cu_seqlens.numel() - 1
+    p.n_rows = _i32_ptr(n_rows, 1)
+    p.rope = _rope(rope)
+    return p
+
+
+def fmha_qk_norm_rope_fwd(q, k, q_out, k_out, *, rope=None, gamma_q=None, gamma_k=None, eps=1e-6, positions=None,
+                          cu_seqlens=None, n_rows=None):
+    """Norm (where a gamma is given) and rotation of every head of q [T, Hq, D] and k [T, Hk, D] into q_out, k_out
+    (which may be q, k themselves; either pair may be None).  rope = (inv_freq, layout, magnitude); the positions
+    come from `positions` (int32 [T]) or from cu_seqlens."""
+    p = _qk_params(q, k, rope, gamma_q, gamma_k, eps, positions, cu_seqlens, n_rows)
+    if q is not None:
+        _same_kind(q, q_out)
+        p.q_stride, p.q_out_stride = _tok_stride(q), _tok_stride(q_out)
+    if k is not None:
+        _same_kind(k, k_out)
+        p.k_stride, p.k_out_stride = _tok_stride(k), _tok_stride(k_out)
+    _check(lib().fmha_qk_norm_rope_fwd(ctypes.byref(p), _opt_ptr(q), _opt_ptr(k), _opt_ptr(q_out), _opt_ptr(k_out),
+                                       _stream()))
+
+
+def fmha_qk_norm_rope_bwd_workspace_size(rows: int, q_heads: int, k_heads: int, head_dim: int) -> int:
+    return int(lib().fmha_qk_norm_rope_bwd_workspace_size(rows, q_heads, k_heads, head_dim))
+
+
+def alloc_qk_norm_rope_workspace(rows: int, q_heads: int, k_heads: int, head_dim: int, device="cuda"):
+    n = fmha_qk_norm_rope_bwd_workspace_size(rows, q_heads, k_heads, head_dim)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def fmha_qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, dgamma_q, dgamma_k, workspace, *, rope=None, gamma_q=None,
+                          gamma_k=None, eps=1e-6, positions=None, cu_seqlens=None, n_rows=None):
+    """Backward of fmha_qk_norm_rope_fwd from the gradients dq_out, dk_out and the forward's inputs q, k (None where
+    there is no gamma); fills dq, dk (which may be dq_out, dk_out) and dgamma_q, dgamma_k (None without a gamma)."""
+    p = _qk_params(dq_out, dk_out, rope, gamma_q, gamma_k, eps, positions, cu_seqlens, n_rows)
+    if dq_out is not None:
+        _same_kind(dq_out, dq, q)
+        p.q_out_stride, p.dq_stride = _tok_stride(dq_out), _tok_stride(dq)
+        p.q_stride = _tok_stride(q) if q is not None else 0
+    if dk_out is not None:
+        _same_kind(dk_out, dk, k)
+        p.k_out_stride, p.dk_stride = _tok_stride(dk_out), _tok_stride(dk)
+        p.k_stride = _tok_stride(k) if k is not None else 0
+    _check(lib().fmha_qk_norm_rope_bwd(ctypes.byref(p), _opt_ptr(dq_out), _opt_ptr(dk_out), _opt_ptr(q), _opt_ptr(k),
+                                       _opt_ptr(dq), _opt_ptr(dk), _gamma_ptr(dgamma_q, p.head_dim),
+                                       _gamma_ptr(dgamma_k, p.head_dim), _opt_ptr(workspace),
+                                       0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                       _stream()))
+
+
+def _cache(k_cache, v_cache, block_table, seqlens):
+    """k_cache, v_cache [num_pages, kv_heads, page_size, D], a page contiguous; block_table int32 [batch, max_pages];
+    seqlens int32 [batch] -> fmha_cache_t"""
+    ks, vs, shape = k_cache.stride(), v_cache.stride(), k_cache.shape
+    assert shape == v_cache.shape and len(shape) == 4 and k_cache.dtype == v_cache.dtype and k_cache.is_cuda and v_cache.is_cuda
+    assert ks == vs or shape[0] <= 1
+    assert ks[1:] == vs[1:] == (shape[2] * shape[3], shape[3], 1), "a page is [kv_heads, page_size, D], contiguous"
+    assert block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous() and block_table.is_cuda
+    assert seqlens.dtype == torch.int32 and seqlens.is_contiguous() and seqlens.is_cuda and seqlens.numel() == block_table.shape[0]
+    c = Cache()
+    c.batch, c.max_pages = block_table.shape
+    c.num_pages, c.kv_heads, c.page_size, c.head_dim = shape
+    c.dtype = _dtype_code(k_cache)
+    c.page_stride = ks[0] if shape[0] > 1 else 0
+    c.block_table, c.seqlens = block_table.data_ptr(), seqlens.data_ptr()
+    return c
+
+
+def fmha_cache_append(k, v, k_cache, v_cache, block_table, seqlens, *, cu_seqlens=None, q=None, q_out=None, rope=None,
+                      gamma_q=None, gamma_k=None, eps=1e-6):
+    """Puts the newest tokens' keys (normed, rotated by their position) and values into the paged cache; `seqlens`
+    counts them already.  k, v [T, kv_heads, D]: rows cu_seqlens[b] .. cu_seqlens[b+1]-1 are the last tokens of
+    sequence b, without cu_seqlens row b is the last token of sequence b.  q [T, heads, D], if given, is treated like
+    k and written to q_out (which may be q)."""
+    c = _cache(k_cache, v_cache, block_table, seqlens)
+    p = AppendParams()
+    p.rows = k.shape[0]
+    assert k.shape == v.shape and k.shape[1:] == (c.kv_heads, c.head_dim) and k.dtype == v.dtype == k_cache.dtype
+    assert cu_seqlens is None or cu_seqlens.numel() == c.batch + 1
+    p.eps = float(eps)
+    p.k_stride, p.v_stride = _tok_stride(k), _tok_stride(v)
+    if q is not None:
+        assert q.shape[0] == k.shape[0] and q.shape[2] == k.shape[2] and q.dtype == k.dtype
+        _same_kind(q, q_out)
+        p.q_heads = q.shape[1]
+        p.q_stride, p.q_out_stride = _tok_stride(q), _tok_stride(q_out)
+    p.gamma_q, p.gamma_k = _gamma_ptr(gamma_q, c.head_dim), _gamma_ptr(gamma_k, c.head_dim)
+    p.cu_seqlens = _i32_ptr(cu_seqlens)
+    p.rope = _rope(rope)
+    _check(lib().fmha_cache_append(ctypes.byref(c), ctypes.byref(p), _opt_ptr(q), k.data_ptr(), v.data_ptr(),
+                                   _opt_ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), _stream()))
