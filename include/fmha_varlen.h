@@ -448,7 +448,7 @@ typedef struct fmha_cache {
   int32_t dtype;     /* fmha_dtype_t */
   int32_t page_size; /* a power of two, at most 65536 */
   int32_t num_pages; /* pages that k and v hold */
-  int32_t max_pages; /* columns of block_table */
+  int32_t max_pages; /* columns of block_table; max_pages * page_size at most 2^30 */
   int64_t page_stride;        /* elements between pages, 0 = dense; a multiple of 8 */
   const int32_t* block_table; /* device, [batch, max_pages] */
   const int32_t* seqlens;     /* device, [batch]: tokens of each sequence, the newest among them */
@@ -473,6 +473,20 @@ typedef struct fmha_append_params {
  * one of them stays, or parts of both. */
 int fmha_cache_append(const fmha_cache_t* c, const fmha_append_params_t* p, const void* q, const void* k, const void* v,
                       void* q_out, void* k_cache, void* v_cache, void* stream);
+
+/* Attention of one query token per sequence over its cache: O = softmax(scale q K^T) V over the keys 0 .. seqlens[b]-1 (the
+ * query's own among them, if it was appended before), lse its log-sum-exp.  A sequence without a key gets o = 0, lse = -inf.
+ *   q, o : device, [batch, heads, head_dim], q_stride / o_stride elements between sequences (0 = dense)
+ *   lse  : device, fp32 [batch, heads] (written)
+ *   head_dim 64 or 128.  max_seqlen: upper bound on seqlens, or <= 0: max_pages * page_size.  It decides how the cache is
+ *   split over workgroups; a wrong value costs time, not correctness.
+ *   workspace: device, 256-byte aligned, fmha_cache_attention_workspace_size bytes (0 for calls that need no splitting: then it
+ *   may be NULL); calls that may overlap in time need workspaces of their own.
+ * One launch, or two where the keys of a sequence are split. */
+size_t fmha_cache_attention_workspace_size(int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_seqlen);
+int fmha_cache_attention(const fmha_cache_t* c, int32_t heads, int32_t max_seqlen, float scale, const void* q, int64_t q_stride,
+                         const void* k_cache, const void* v_cache, void* o, int64_t o_stride, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 /* Number of 128-row tiles the schedule holds at most for this shape (host
  * arithmetic), and a device-to-host-free way for tests to locate the tile list

@@ -5,35 +5,21 @@
 
 #include <cmath>
 
-#include "../../include/fmha_varlen.h"
-#include "host_error.h"
+#include "host_checks.h"
 #include "qk_rows_kernels.h"
 
 namespace {
 
 using fmha_host::fail;
 
-bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-
-int check_ptr(const char* name, const void* ptr, size_t align) {
-  if (!ptr) return fail(FMHA_ERR_INVALID_ARG, "%s is null", name);
-  if (misaligned(ptr, align)) return fail(FMHA_ERR_INVALID_ARG, "%s is not %zu-byte aligned", name, align);
-  return FMHA_OK;
-}
-
-int check_stride(const char* name, int64_t s, int64_t dense, int64_t* out) {
-  if (s == 0) s = dense;
-  if (s < dense || (s & 7) || s > ((int64_t)1 << 24))
-    return fail(FMHA_ERR_INVALID_ARG, "%s_stride=%lld must be 0 or a multiple of 8 from heads*head_dim=%lld to 2^24", name,
-                (long long)s, (long long)dense);
-  *out = s;
-  return FMHA_OK;
-}
+using fmha_host::check_ptr;
+using fmha_host::check_stride;
+using fmha_host::misaligned;
 
 // What all of the entry points have: sizes, dtype, norm, rotation.
 int check_heads(int32_t q_heads, int32_t k_heads, int32_t head_dim, int32_t dtype, float eps, const float* gamma_q,
                 const float* gamma_k, const fmha_rope_t* rope, fmha::QkRows* a) {
-  if (dtype != FMHA_F16 && dtype != FMHA_BF16) return fail(FMHA_ERR_UNSUPPORTED, "dtype=%d is neither FMHA_F16 nor FMHA_BF16", dtype);
+  if (int rc = fmha_host::check_dtype(dtype)) return rc;
   if (q_heads < 0 || k_heads < 0 || q_heads > 65536 || k_heads > 65536)
     return fail(FMHA_ERR_INVALID_ARG, "%d query heads, %d key heads: invalid numbers", q_heads, k_heads);
   if (head_dim <= 0 || (head_dim & 15)) return fail(FMHA_ERR_INVALID_ARG, "head_dim=%d must be a positive multiple of 16", head_dim);
@@ -267,18 +253,11 @@ int fmha_cache_append(const fmha_cache_t* c, const fmha_append_params_t* p, cons
   fmha::QkRows a;
   int rc = check_heads(p->q_heads, c->kv_heads, c->head_dim, c->dtype, p->eps, p->gamma_q, p->gamma_k, &p->rope, &a);
   if (rc) return rc;
-  if (c->kv_heads < 1) return fail(FMHA_ERR_INVALID_ARG, "kv_heads=%d must be positive", c->kv_heads);
-  if (c->batch < 0) return fail(FMHA_ERR_INVALID_ARG, "batch=%d is negative", c->batch);
+  int64_t page_stride;
+  if ((rc = fmha_host::check_cache(c, &page_stride))) return rc;
   if (p->rows < 0) return fail(FMHA_ERR_INVALID_ARG, "rows=%d is negative", p->rows);
   if (!p->cu_seqlens && p->rows != c->batch)
     return fail(FMHA_ERR_INVALID_ARG, "rows=%d differs from batch=%d, and there are no cu_seqlens", p->rows, c->batch);
-  if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
-    return fail(FMHA_ERR_INVALID_ARG, "page_size=%d must be a power of two, at most 65536", c->page_size);
-  if (c->num_pages < 0 || c->max_pages < 0) return fail(FMHA_ERR_INVALID_ARG, "num_pages=%d, max_pages=%d: negative", c->num_pages, c->max_pages);
-  const int64_t dense = (int64_t)c->kv_heads * c->page_size * c->head_dim;
-  if (c->page_stride && (c->page_stride < dense || (c->page_stride & 7)))
-    return fail(FMHA_ERR_INVALID_ARG, "page_stride=%lld must be 0 or a multiple of 8 that is >= kv_heads*page_size*head_dim=%lld",
-                (long long)c->page_stride, (long long)dense);
   const int64_t dense_q = (int64_t)p->q_heads * c->head_dim, dense_k = (int64_t)c->kv_heads * c->head_dim;
   int64_t v_stride;
   if ((rc = check_stride("q", p->q_stride, dense_q, &a.q_stride)) || (rc = check_stride("k", p->k_stride, dense_k, &a.k_stride)) ||
@@ -286,10 +265,7 @@ int fmha_cache_append(const fmha_cache_t* c, const fmha_append_params_t* p, cons
     return rc;
   fmha_host::g_err[0] = 0;
   if (p->rows == 0 || c->batch == 0) return FMHA_OK;
-  if ((rc = check_ptr("k", k, 16)) || (rc = check_ptr("v", v, 16)) || (rc = check_ptr("k_cache", k_cache, 16)) ||
-      (rc = check_ptr("v_cache", v_cache, 16)) || (rc = check_ptr("block_table", c->block_table, 4)) ||
-      (rc = check_ptr("seqlens", c->seqlens, 4)))
-    return rc;
+  if ((rc = check_ptr("k", k, 16)) || (rc = check_ptr("v", v, 16)) || (rc = fmha_host::check_cache_pointers(c, k_cache, v_cache))) return rc;
   if (p->q_heads && ((rc = check_ptr("q", q, 16)) || (rc = check_ptr("q_out", q_out, 16)))) return rc;
   if (misaligned(p->cu_seqlens, 4)) return fail(FMHA_ERR_INVALID_ARG, "cu_seqlens must be 4-byte aligned");
   a.rows = p->rows;
@@ -305,8 +281,8 @@ int fmha_cache_append(const fmha_cache_t* c, const fmha_append_params_t* p, cons
   a.batch = c->batch;
   a.seqlens = c->seqlens;
   a.table = c->block_table;
-  a.page_stride = c->page_stride ? c->page_stride : dense;
-  while ((1 << a.page_shift) < c->page_size) a.page_shift++;
+  a.page_stride = page_stride;
+  a.page_shift = fmha_host::page_shift(c);
   a.num_pages = c->num_pages;
   a.max_pages = c->max_pages;
   const unsigned grid = cut(&a);

@@ -34,6 +34,7 @@ EXPORTS = ("fmha_varlen_workspace_size", "fmha_varlen_fwd", "fmha_varlen_bwd",
            "fmha_embedding_bwd_sorted",
            "fmha_rope_frequencies", "fmha_qk_norm_rope_fwd", "fmha_qk_norm_rope_bwd",
            "fmha_qk_norm_rope_bwd_workspace_size", "fmha_cache_append",
+           "fmha_cache_attention", "fmha_cache_attention_workspace_size",
            "fmha_varlen_schedule_info", "fmha_last_error")
 
 
@@ -171,6 +172,11 @@ def lib():
         L.fmha_qk_norm_rope_bwd.restype = ctypes.c_int
         L.fmha_cache_append.argtypes = [cp, ctypes.POINTER(AppendParams)] + [vp] * 7
         L.fmha_cache_append.restype = ctypes.c_int
+        L.fmha_cache_attention_workspace_size.argtypes = [i32] * 5
+        L.fmha_cache_attention_workspace_size.restype = ctypes.c_size_t
+        L.fmha_cache_attention.argtypes = [cp, i32, i32, ctypes.c_float, vp, ctypes.c_int64, vp, vp, vp, ctypes.c_int64, vp, vp,
+                                           ctypes.c_size_t, vp]
+        L.fmha_cache_attention.restype = ctypes.c_int
         L.fmha_varlen_schedule_info.argtypes = [ctypes.c_int32] * 3 + [ctypes.POINTER(ctypes.c_size_t)] * 2
         L.fmha_varlen_schedule_info.restype = ctypes.c_int32
         L.fmha_last_error.restype = ctypes.c_char_p
@@ -619,3 +625,26 @@ def fmha_cache_append(k, v, k_cache, v_cache, block_table, seqlens, *, cu_seqlen
     p.rope = _rope(rope)
     _check(lib().fmha_cache_append(ctypes.byref(c), ctypes.byref(p), _opt_ptr(q), k.data_ptr(), v.data_ptr(),
                                    _opt_ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), _stream()))
+
+
+def fmha_cache_attention_workspace_size(batch: int, heads: int, kv_heads: int, head_dim: int, max_seqlen: int) -> int:
+    return int(lib().fmha_cache_attention_workspace_size(batch, heads, kv_heads, head_dim, max_seqlen))
+
+
+def alloc_cache_attention_workspace(batch: int, heads: int, kv_heads: int, head_dim: int, max_seqlen: int, device="cuda"):
+    """A workspace for calls with these sizes, or None where they need none."""
+    n = fmha_cache_attention_workspace_size(batch, heads, kv_heads, head_dim, max_seqlen)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def fmha_cache_attention(q, k_cache, v_cache, block_table, seqlens, max_seqlen, scale, o, lse, workspace):
+    """One query token per sequence, q [batch, heads, D], against its seqlens[b] keys in the paged cache; fills o and
+    lse (fp32 [batch, heads])."""
+    c = _cache(k_cache, v_cache, block_table, seqlens)
+    assert q.shape[0] == c.batch and q.shape[2] == c.head_dim and q.dtype == k_cache.dtype
+    _same_kind(q, o)
+    assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == c.batch * q.shape[1]
+    _check(lib().fmha_cache_attention(ctypes.byref(c), q.shape[1], int(max_seqlen), float(scale), q.data_ptr(), _tok_stride(q),
+                                      k_cache.data_ptr(), v_cache.data_ptr(), o.data_ptr(), _tok_stride(o), lse.data_ptr(),
+                                      _opt_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                      _stream()))

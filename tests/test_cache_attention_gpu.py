@@ -1,0 +1,210 @@
+"""Attention of one token per sequence over a paged cache, against the definition in float64 on the CPU.
+
+Tolerances: o is off by the rounding of its value (eps / 2 relative) and by that of the probabilities before the second
+product, at most eps / 2 of each and for fp16 at most 2^-25 of the largest where they are subnormal; fp32 scores of
+magnitude s shift a probability by s 2^-22, counted as 2^-16 of the sum of p |v|.  lse is fp32: 2^-20 (1 + |lse|)."""
+import math
+
+import pytest
+import torch
+
+from paper_2208_08124_amd import fmha
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def make_cache(lens, heads, kv_heads, d, page, dtype, seed=0, extra_columns=0, between=0, spread=1.0):
+    """Pages in random order, NaN in every place that no sequence holds."""
+    g = torch.Generator().manual_seed(seed)
+    b = len(lens)
+    cols = max(1, -(-max(lens) // page)) + extra_columns
+    counts = [-(-n // page) for n in lens]
+    pages = sum(counts) + 1
+    order = torch.randperm(pages, generator=g).tolist()
+    table = torch.full((b, cols), -7, dtype=torch.int32)
+    full = [torch.full((pages, 1 + between, kv_heads, page, d), float("nan"), dtype=DT[dtype]) for _ in range(2)]
+    ks, vs = [], []
+    for i, n in enumerate(lens):
+        mine = [order.pop() for _ in range(counts[i])]
+        table[i, :counts[i]] = torch.tensor(mine, dtype=torch.int32)
+        k, v = ((torch.randn(n, kv_heads, d, generator=g) * spread).to(DT[dtype]) for _ in range(2))
+        for j, pg in enumerate(mine):
+            rows = slice(j * page, min(n, (j + 1) * page))
+            full[0][pg, 0, :, :rows.stop - rows.start] = k[rows].transpose(0, 1)
+            full[1][pg, 0, :, :rows.stop - rows.start] = v[rows].transpose(0, 1)
+        ks.append(k)
+        vs.append(v)
+    q = torch.randn(b, heads, d, generator=g).to(DT[dtype])
+    dev = [x.cuda() for x in full]
+    return dict(q=q, ks=ks, vs=vs, full=dev, k_cache=dev[0][:, 0], v_cache=dev[1][:, 0], table=table.cuda(),
+                seqlens=torch.tensor(lens, dtype=torch.int32, device="cuda"), heads=heads, kv_heads=kv_heads, dtype=DT[dtype])
+
+
+def check(s, o, lse, scale, lens=None, skip=lambda b, j: False):
+    g = s["heads"] // s["kv_heads"]
+    half = torch.finfo(s["dtype"]).eps / 2
+    tiny = 2.0 ** -25 if s["dtype"] == torch.float16 else 0.0
+    for b, (k, v) in enumerate(zip(s["ks"], s["vs"])):
+        n = k.shape[0] if lens is None else lens[b]
+        keep = [j for j in range(n) if not skip(b, j)]
+        k, v = k.double()[keep], v.double()[keep]
+        for h in range(s["heads"]):
+            got, got_lse = o[b, h].double().cpu(), float(lse[b, h])
+            if not keep:
+                assert (got == 0).all() and got_lse == -math.inf, (b, h)
+                continue
+            score = k[:, h // g] @ s["q"][b, h].double() * scale
+            want = float(torch.logsumexp(score, 0))
+            p = torch.exp(score - want)
+            vv = v[:, h // g]
+            ref, mag = p @ vv, p @ vv.abs()
+            tol = ref.abs() * half + mag * (half + 2.0 ** -16) + tiny * vv.abs().sum(0) * math.exp(float(score.max()) - want) + 1e-7
+            assert ((got - ref).abs() <= tol).all(), (b, h, float(((got - ref).abs() - tol).max()))
+            assert abs(got_lse - want) <= 2.0 ** -20 * (1 + abs(want) + float(score.abs().max())), (b, h, got_lse, want)
+
+
+def call(s, scale, longest, workspace="own", **over):
+    o = torch.full(s["q"].shape, float("nan"), dtype=s["dtype"], device="cuda")
+    lse = torch.full(s["q"].shape[:2], float("nan"), device="cuda")
+    b, h, d = s["q"].shape
+    ws = fmha.alloc_cache_attention_workspace(b, h, s["kv_heads"], d, longest)
+    fmha.fmha_cache_attention(s["q"].cuda(), s["k_cache"], s["v_cache"], over.get("table", s["table"]),
+                              over.get("seqlens", s["seqlens"]), longest, scale, o, lse, ws)
+    return o, lse
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("case", [
+    # lens, heads, kv_heads, D, page, unrelated pages between
+    ([1], 1, 1, 64, 16, 0),
+    ([1, 0, 31, 32, 33], 4, 4, 64, 16, 0),
+    ([127, 128, 129, 255, 256, 257], 8, 2, 128, 64, 1),
+    ([300, 5], 12, 1, 64, 1, 0),
+    ([300, 5, 77], 32, 8, 128, 8, 0),
+    ([513, 1000], 40, 2, 64, 32, 0),      # 20 heads in a group: two tiles of columns
+    ([513, 100], 17, 1, 128, 128, 0),
+    ([4000, 17, 0, 1], 6, 2, 128, 16, 0),
+    ([2], 64, 1, 128, 2, 0),
+], ids=lambda c: "%d_of_%d_%d-%d_of_%d_page_%d" % (len(c[0]), max(c[0]), *c[1:5]))
+def test_against_the_definition(case, dtype):
+    lens, heads, kv_heads, d, page, between = case
+    s = make_cache(lens, heads, kv_heads, d, page, dtype, between=between, extra_columns=1)
+    check(s, *call(s, d ** -0.5, max(lens)), d ** -0.5)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64)])
+def test_a_long_context_and_wrong_bounds(dtype, d):
+    """Split over many workgroups; the stated bound may be too small, too large or missing."""
+    lens = [30000, 1, 777]
+    s = make_cache(lens, 8, 2, d, 64, dtype)
+    for longest in (max(lens), 100, 1, 200000):
+        check(s, *call(s, d ** -0.5, longest), d ** -0.5)
+    o = torch.empty(s["q"].shape, dtype=s["dtype"], device="cuda")
+    lse = torch.empty(s["q"].shape[:2], device="cuda")
+    cap = s["table"].shape[1] * 64
+    fmha.fmha_cache_attention(s["q"].cuda(), s["k_cache"], s["v_cache"], s["table"], s["seqlens"], 0, d ** -0.5, o, lse,
+                              fmha.alloc_cache_attention_workspace(3, 8, 2, d, cap))
+    check(s, o, lse, d ** -0.5)
+    again = call(s, d ** -0.5, max(lens))
+    for _ in range(3):
+        assert all(torch.equal(x, y) for x, y in zip(again, call(s, d ** -0.5, max(lens))))
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+def test_scales(scale):
+    s = make_cache([1500, 40], 4, 2, 64, 16, "bf16")
+    check(s, *call(s, scale, 1500), scale)
+
+
+def test_scores_that_climb():
+    """Each block's maximum above all before: every one rescales what was summed up."""
+    s = make_cache([2000], 2, 1, 64, 32, "f16")
+    rise = torch.linspace(0, 40, 2000)
+    k = s["ks"][0].clone()
+    k[:, 0] = (rise[:, None] * s["q"][0, 0].float() / s["q"][0, 0].float().square().sum() * 8).half()
+    s["ks"][0] = k
+    for j in range(2000):
+        s["k_cache"][int(s["table"][0, j // 32]), :, j % 32] = k[j].cuda()
+    check(s, *call(s, 0.125, 2000), 0.125)
+
+
+def test_pages_that_are_none():
+    """Numbers outside the cache name no page, tokens behind the table do not exist, lengths below zero are none."""
+    page, lens = 16, [100, 64, 40, 30]
+    s = make_cache(lens, 4, 2, 128, page, "bf16")
+    table = s["table"].clone()
+    table[0, 2], table[1, 0], table[1, 3] = -1, s["k_cache"].shape[0], 2 ** 31 - 1
+    table[2, :] = -5
+    bad = {0: {2}, 1: {0, 3}, 2: {0, 1, 2}, 3: set()}
+    skip = lambda b, j: j // page in bad[b]
+    check(s, *call(s, 0.1, 100, table=table), 0.1, skip=skip)
+    seqlens = s["seqlens"].clone()
+    seqlens[0] = 5000  # behind the table: page 6 is a quarter full, the rest of it holds NaN, and page numbers end at 7
+    seqlens[3] = -3
+    cut = table[:, :6].contiguous()
+    check(s, *call(s, 0.1, 100, table=cut, seqlens=seqlens), 0.1, lens=[96, 64, 40, 0], skip=skip)
+
+
+def test_a_cache_beyond_32_bits():
+    kv, page, d, pages = 8, 64, 128, 34000  # 4.5 GB each
+    k_cache, v_cache = (torch.zeros(pages, kv, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    g = torch.Generator().manual_seed(1)
+    k, v = (torch.randn(page, kv, d, generator=g).to(torch.bfloat16) for _ in range(2))
+    k_cache[-1], v_cache[-1] = k.transpose(0, 1).cuda(), v.transpose(0, 1).cuda()
+    s = dict(q=torch.randn(1, 16, d, generator=g).to(torch.bfloat16), ks=[k], vs=[v], k_cache=k_cache, v_cache=v_cache, heads=16, kv_heads=kv,
+             dtype=torch.bfloat16, table=torch.tensor([[pages - 1]], dtype=torch.int32, device="cuda"),
+             seqlens=torch.tensor([page], dtype=torch.int32, device="cuda"))
+    check(s, *call(s, 0.1, page), 0.1)
+
+
+def test_strided_queries_and_outputs():
+    s = make_cache([50, 9, 300], 4, 4, 64, 16, "f16")
+    wide = torch.full((3, 3 * 256 + 8), 5.0, dtype=torch.float16, device="cuda")
+    q, o = wide[:, :256].unflatten(1, (4, 64)), wide[:, 512:768].unflatten(1, (4, 64))
+    q.copy_(s["q"])
+    lse = torch.empty(3, 4, device="cuda")
+    fmha.fmha_cache_attention(q, s["k_cache"], s["v_cache"], s["table"], s["seqlens"], 300, 0.125, o, lse,
+                              fmha.alloc_cache_attention_workspace(3, 4, 4, 64, 300))
+    check(s, o, lse, 0.125)
+    assert (wide[:, 256:512] == 5).all() and (wide[:, 768:] == 5).all()
+
+
+def test_two_streams_and_captured_graphs():
+    """Calls on two streams at once, each with a workspace of its own; two graphs replayed with growing lengths."""
+    cases = [make_cache([3000, 200], 8, 2, 128, 16, "bf16", seed=i) for i in range(2)]
+    want = [call(s, 0.09, 3000) for s in cases]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    bufs = []
+    for s in cases:
+        b, h, d = s["q"].shape
+        bufs.append(dict(q=s["q"].cuda(), o=torch.empty(b, h, d, dtype=s["dtype"], device="cuda"), lse=torch.empty(b, h, device="cuda"),
+                         ws=fmha.alloc_cache_attention_workspace(b, h, 2, d, 3000)))
+
+    def run(i):
+        s, f = cases[i], bufs[i]
+        fmha.fmha_cache_attention(f["q"], s["k_cache"], s["v_cache"], s["table"], s["seqlens"], 3000, 0.09, f["o"], f["lse"], f["ws"])
+
+    torch.cuda.synchronize()
+    for i in range(2):
+        with torch.cuda.stream(streams[i]):
+            run(i)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(bufs[i]["o"], want[i][0]) and torch.equal(bufs[i]["lse"], want[i][1])
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for i in range(2):
+        with torch.cuda.graph(graphs[i], stream=streams[i]):
+            run(i)
+    for lens in ([1, 0], [1000, 199], [3000, 200]):
+        for i in range(2):
+            cases[i]["seqlens"].copy_(torch.tensor(lens, dtype=torch.int32))
+        want = [call(s, 0.09, 3000) for s in cases]
+        torch.cuda.synchronize()
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(bufs[i]["o"], want[i][0]) and torch.equal(bufs[i]["lse"], want[i][1])

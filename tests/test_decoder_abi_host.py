@@ -130,7 +130,7 @@ def append(fmha, **over):
 
 CACHE_REFUSALS = [(dict(batch=-1), "batch"), (dict(kv_heads=0), "kv_heads"), (dict(page_size=0), "page_size"), (dict(page_size=24), "page_size"),
                   (dict(page_size=1 << 17), "page_size"), (dict(num_pages=-1), "num_pages"), (dict(max_pages=-1), "max_pages"),
-                  (dict(page_stride=1024), "page_stride"), (dict(page_stride=2 * 16 * 64 + 4), "page_stride"),
+                  (dict(max_pages=(1 << 26) + 1), "max_pages"), (dict(page_stride=1024), "page_stride"), (dict(page_stride=2 * 16 * 64 + 4), "page_stride"),
                   (dict(block_table=None), "block_table"), (dict(seqlens=None), "seqlens"), (dict(seqlens=P + 2), "seqlens")]
 
 
@@ -152,3 +152,23 @@ def test_append_refusals():
         assert run(cache(fmha), append(fmha), *a) == INV, i
     assert lib.fmha_cache_append(None, ctypes.byref(append(fmha)), *[P] * 6, None) == INV
     assert run(cache(fmha, batch=0), append(fmha, rows=0), *[None] * 6) == 0
+
+
+def test_cache_attention_refusals():
+    from paper_2208_08124_amd import fmha
+    lib, (INV, UNS, WS) = fmha.lib(), (fmha.FMHA_ERR_INVALID_ARG, fmha.FMHA_ERR_UNSUPPORTED, fmha.FMHA_ERR_WORKSPACE)
+
+    def run(c, heads=4, longest=4096, scale=0.125, q=P, qs=0, k=P, v=P, o=P, os_=0, lse=P, ws=P, nws=1 << 30):
+        return lib.fmha_cache_attention(ctypes.byref(c) if c else None, heads, longest, scale, q, qs, k, v, o, os_, lse, ws, nws, None)
+
+    for over, frag in CACHE_REFUSALS:
+        assert run(cache(fmha, **over)) == INV and frag in fmha.last_error(), (over, fmha.last_error())
+    assert run(None) == INV and run(cache(fmha, dtype=9)) == UNS and run(cache(fmha, head_dim=96)) == UNS
+    for over in (dict(heads=3), dict(heads=0), dict(heads=-2), dict(scale=float("nan")), dict(scale=float("inf")), dict(qs=128), dict(os_=260),
+                 dict(q=None), dict(o=None), dict(lse=None), dict(k=None), dict(v=None), dict(q=P + 2), dict(lse=P + 1)):
+        assert run(cache(fmha), **over) == INV, over
+    assert run(cache(fmha), ws=None) == WS and run(cache(fmha), ws=P + 16) == WS and run(cache(fmha), nws=64) == WS
+    assert run(cache(fmha, batch=0), q=None, k=None, v=None, o=None, lse=None, ws=None) == 0
+    f = fmha.fmha_cache_attention_workspace_size
+    assert f(2, 4, 3, 64, 100) == 0 and f(2, 4, 2, 96, 100) == 0 and f(2, 4, 2, 64, -1) == 0
+    assert f(2, 4, 2, 64, 100) == 0 and f(2, 4, 2, 64, 100000) > 0  # one workgroup each, and several
