@@ -488,6 +488,36 @@ int fmha_cache_attention(const fmha_cache_t* c, int32_t heads, int32_t max_seqle
                          const void* k_cache, const void* v_cache, void* o, int64_t o_stride, float* lse, void* workspace,
                          size_t workspace_bytes, void* stream);
 
+/* ---- Causal attention with grouped heads ------------------------------------------
+ * As fmha_varlen_fwd / _bwd, but query i of a sequence attends keys 0 .. i of it, and key / value heads are shared:
+ *   q, o, d_o, dq : device [T, heads, head_dim];  k, v, dk, dv : device [T, kv_heads, head_dim];  lse : fp32 [heads, T]
+ *   dK, dV sum over the query heads that share them, in fp32 and in a fixed order: results repeat bit for bit.
+ * Rows at and beyond cu_seqlens[batch] are neither read nor written.  The backward needs the forward's o and lse, and a
+ * workspace sized with need_bwd. */
+typedef struct fmha_causal_params {
+  int32_t batch;        /* as in fmha_varlen_params_t */
+  int32_t total_tokens; /* rows the tensors hold, >= cu_seqlens[batch] */
+  int32_t heads;
+  int32_t kv_heads;     /* divides heads */
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t max_seqlen;   /* upper bound on the longest sequence, or <= 0 if unknown; a wrong value costs time, not correctness */
+  int32_t dtype;        /* fmha_dtype_t */
+  uint32_t flags;       /* FMHA_FLAG_REUSE_SCHEDULE or 0 */
+  float scale;
+  int64_t q_stride, k_stride, v_stride, o_stride;
+  int64_t do_stride, dq_stride, dk_stride, dv_stride;
+  const int32_t* cu_seqlens;      /* device, [batch + 1] */
+  const int32_t* cu_seqlens_host; /* optional host copy: lets the call validate the prefix sums */
+  void* workspace;                /* device, 256-byte aligned */
+  size_t workspace_bytes;
+} fmha_causal_params_t;
+
+size_t fmha_causal_workspace_size(int32_t batch, int32_t total_tokens, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                  int32_t need_bwd);
+int fmha_causal_fwd(const fmha_causal_params_t* p, const void* q, const void* k, const void* v, void* o, float* lse, void* stream);
+int fmha_causal_bwd(const fmha_causal_params_t* p, const void* q, const void* k, const void* v, const void* o, const void* d_o,
+                    const float* lse, void* dq, void* dk, void* dv, void* stream);
+
 /* Number of 128-row tiles the schedule holds at most for this shape (host
  * arithmetic), and a device-to-host-free way for tests to locate the tile list
  * inside the workspace: the list starts at byte offset *list_offset and holds

@@ -1,0 +1,277 @@
+// Causal backward on packed sequences with grouped heads, by recomputation, in two passes without atomics:
+//   dQ pass    per tile of 128 queries and query head: D = rowsum(dO o O), and for every block of keys up to the diagonal
+//              S^T = K Q^T,  dP^T = V dO^T,  P^T = exp(S^T - LSE),  dS^T = P^T o (dP^T - D),  dQ^T += K^T dS^T
+//   dK/dV pass per tile of 128 keys and key head: for every query head that shares it and every block of queries from the
+//              diagonal on  S = Q K^T,  dP = dO V^T,  P, dS as above,  dV^T += dO^T P,  dK^T += Q^T dS
+// so that the sums over a group's heads stay in the registers of one wavefront, in fp32 and in a fixed order.
+// The orientations are chosen so that P and dS go back into the matrix cores as operands without passing through LDS.
+#pragma once
+#include "causal_fwd_kernel.h"
+
+namespace fmha {
+
+template <typename T>
+__device__ __forceinline__ u32x4 pack_half(const float (&x)[16], int t2) {
+  return u32x4{Op<T>::pack2(x[8 * t2], x[8 * t2 + 1]), Op<T>::pack2(x[8 * t2 + 2], x[8 * t2 + 3]),
+               Op<T>::pack2(x[8 * t2 + 4], x[8 * t2 + 5]), Op<T>::pack2(x[8 * t2 + 6], x[8 * t2 + 7])};
+}
+
+// ------------------------------------------------------------------ dQ
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void causal_dq_kernel(const CausalArgs a) {
+  constexpr int NST = kCausalStages<D>, NT = D / 16, NC = D / 32;
+  constexpr uint32_t kHalfBytes = kCausalKeys * D * 2;
+  constexpr int kPieces = 2 * (D / 64) * 2;
+  __shared__ __align__(1024) CausalFwdLds<T, D> lds;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+  const RowRead rr(ln, g);
+  const ColRead cr(lane);
+  const uint32_t ring_addr = lds_addr(&lds.ring[0][0][0]);
+  const float c2 = a.scale * kLog2e;
+  // "row past the end" in the dK/dV pass: its probabilities vanish
+  if (blockIdx.x == 0 && tid == 0) {
+    a.lse2[(int64_t)a.heads * a.total] = INFINITY;
+    a.dsum[(int64_t)a.heads * a.total] = 0.f;
+  }
+  for (int item = blockIdx.x;; item += gridDim.x) {
+    const int rank = item / a.heads;
+    const TileItem ti = causal_tile(a, rank);
+    if (ti.len == 0) return;
+    const int head = causal_head(item - rank * a.heads, a.heads, a.kv_heads, a.group), kvh = head / a.group;
+    const int len = ti.len, row0 = ti.row0, w0 = row0 + 32 * wave;
+    const uint16_t* kbase = a.k + (int64_t)ti.r0 * a.k_stride + kvh * D;
+    const uint16_t* vbase = a.v + (int64_t)ti.r0 * a.v_stride + kvh * D;
+    const int keys = min(len, row0 + kTileRows), n = (keys + kCausalKeys - 1) / kCausalKeys;
+    const int mine = w0 < len ? w0 / kCausalKeys + 1 : 0;
+    auto request = [&](int kt, int stage) {
+      const uint32_t at = ring_addr + stage * (2 * kHalfBytes);
+      dma_block<D, kCausalKeys>(kbase, a.k_stride, kt * kCausalKeys, len - 1, wave, at);
+      dma_block<D, kCausalKeys>(vbase, a.v_stride, kt * kCausalKeys, len - 1, wave, at + kHalfBytes);
+    };
+    request(0, 0);
+    if (NST == 3 && n > 1) request(1, 1);
+
+    // Q^T, dO^T as operands (column = query ln), D of the query, its LSE
+    u32x4 qb[NT], gb[NT];
+    float dsum = 0.f, lse2;
+    {
+      const int64_t tok = ti.r0 + min(w0 + ln, len - 1);
+      const uint16_t* qp = a.q + tok * a.q_stride + head * D + 8 * g;
+      const uint16_t* gp = a.d_o + tok * a.do_stride + head * D + 8 * g;
+      const uint16_t* op = a.o_in + tok * a.o_stride + head * D + 8 * g;
+#pragma unroll
+      for (int t = 0; t < NT; t++) {
+        qb[t] = *reinterpret_cast<const u32x4*>(qp + 16 * t);
+        gb[t] = *reinterpret_cast<const u32x4*>(gp + 16 * t);
+        const u32x4 ov = *reinterpret_cast<const u32x4*>(op + 16 * t);
+#pragma unroll
+        for (int e = 0; e < 4; e++) dsum = Op<T>::dot2(gb[t][e], ov[e], dsum);
+      }
+      dsum += other_half(dsum);
+      lse2 = a.lse[(int64_t)head * a.total + tok] * kLog2e;
+#pragma unroll
+      for (int t = 0; t < NT; t++) asm volatile("" ::"v"(qb[t]), "v"(gb[t]));
+      asm volatile("" ::"v"(dsum), "v"(lse2));
+    }
+    f32x16 dq[NC];
+#pragma unroll
+    for (int cb = 0; cb < NC; cb++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) dq[cb][r] = 0.f;
+
+    int stage = 0;
+    for (int kt = 0; kt < n; kt++) {
+      if (NST == 3 && kt + 1 < n)
+        wait_vmem<kPieces>();
+      else
+        wait_vmem<0>();
+      __syncthreads();
+      const int ahead = NST == 3 ? (stage == 0 ? 2 : stage - 1) : 1 - stage;
+      if (kt + NST - 1 < n) request(kt + NST - 1, ahead);
+      if (kt < mine) {
+        const uint16_t *sK = &lds.ring[stage][0][0], *sV = &lds.ring[stage][1][0];
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++) {
+          const int key0 = kt * kCausalKeys + 32 * kb;
+          if (key0 > w0) break;  // (blocks of 32 line up with the wavefronts' queries)
+          f32x16 s, dp;
+#pragma unroll
+          for (int r = 0; r < 16; r++) s[r] = dp[r] = 0.f;
+#pragma unroll
+          for (int t = 0; t < NT; t++) {
+            s = Op<T>::mfma(read_rows<D, kCausalKeys>(rr, sK, kb, t), qb[t], s);
+            dp = Op<T>::mfma(read_rows<D, kCausalKeys>(rr, sV, kb, t), gb[t], dp);
+          }
+          float ds[16];
+#pragma unroll
+          for (int r = 0; r < 16; r++) ds[r] = fast_exp2(__builtin_fmaf(s[r], c2, -lse2)) * (dp[r] - dsum);
+          if (key0 == w0) {  // the diagonal
+#pragma unroll
+            for (int r = 0; r < 16; r++)
+              if (8 * (r >> 2) + 4 * g + (r & 3) > ln) ds[r] = 0.f;
+          }
+          const u32x4 dsb[2] = {pack_half<T>(ds, 0), pack_half<T>(ds, 1)};
+#pragma unroll
+          for (int t2 = 0; t2 < 2; t2++)
+#pragma unroll
+            for (int cb = 0; cb < NC; cb++) dq[cb] = Op<T>::mfma(read_cols<D, kCausalKeys>(cr, sK, 2 * kb + t2, cb), dsb[t2], dq[cb]);
+        }
+      }
+      stage = NST == 3 ? (stage == 2 ? 0 : stage + 1) : 1 - stage;
+    }
+    __syncthreads();
+    if (mine) {
+      if (lane < 32 && w0 + ln < len) {
+        const int64_t si = (int64_t)head * a.total + ti.r0 + w0 + ln;
+        a.dsum[si] = -dsum;
+        a.lse2[si] = lse2;
+      }
+      uint16_t* scratch = &lds.ring[0][0][0] + 2048 * wave;
+#pragma unroll
+      for (int h = 0; h < D / 64; h++) {
+        const f32x16 x[2] = {dq[2 * h], dq[2 * h + 1]};
+        store_rows32<T>(x, a.scale, scratch, a.dq, (int64_t)(ti.r0 + w0) * a.dq_stride + head * D + 64 * h, a.dq_stride, len - w0);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ dK, dV
+// Queries go by in blocks of 32.  The wavefront's 32 keys: V as operand in registers, K too at 64 channels; at 128 the
+// accumulators leave no room for it and K is read from LDS.
+constexpr int kCausalQueries = 32;
+
+template <int D>
+struct CausalDkvLds {
+  uint16_t k[D == 64 ? 8 : kTileRows * D];  // [64-row half][..]
+  struct alignas(1024) {
+    uint16_t q[kCausalQueries * D], g[kCausalQueries * D];
+    float stat[4][64];  // per wavefront: lse log2(e) of the 32 queries, then -D of them
+  } ring[2];
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void causal_dkv_kernel(const CausalArgs a) {
+  constexpr int NT = D / 16, NC = D / 32;
+  __shared__ __align__(1024) CausalDkvLds<D> lds;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+  const RowRead rr(ln, g);
+  const ColRead cr(lane);
+  const float c2 = a.scale * kLog2e;
+  for (int item = blockIdx.x;; item += gridDim.x) {
+    const int rank = item / a.kv_heads;
+    TileItem ti = causal_tile(a, rank);
+    if (ti.len == 0) return;
+    const int kvh = item - rank * a.kv_heads, len = ti.len;
+    // the tiles' order counts from the sequence's end here
+    const int k0 = ((len + kTileRows - 1) / kTileRows - 1) * kTileRows - ti.row0, w0 = k0 + 32 * wave;
+    const int qt0 = k0 / kCausalQueries, nq = (len + kCausalQueries - 1) / kCausalQueries - qt0, n = nq * a.group;
+    int f_head = kvh * a.group, f_qt = 0;  // what is requested next
+    auto request = [&](int stage) {
+      const int row = (qt0 + f_qt) * kCausalQueries;
+      const uint32_t at = lds_addr(&lds.ring[stage].q[0]);
+      dma_block<D, kCausalQueries>(a.q + (int64_t)ti.r0 * a.q_stride + f_head * D, a.q_stride, row, len - 1, wave, at);
+      dma_block<D, kCausalQueries>(a.d_o + (int64_t)ti.r0 * a.do_stride + f_head * D, a.do_stride, row, len - 1, wave,
+                                   lds_addr(&lds.ring[stage].g[0]));
+      const int q = row + (lane & 31);
+      const int64_t si = q < len ? (int64_t)f_head * a.total + ti.r0 + q : (int64_t)a.heads * a.total;
+      dma4((lane < 32 ? a.lse2 : a.dsum) + si, __builtin_amdgcn_readfirstlane(lds_addr(&lds.ring[stage].stat[wave][0])));
+      if (++f_qt == nq) {
+        f_qt = 0;
+        f_head++;
+      }
+    };
+    if (D == 128) {
+      const uint16_t* kbase = a.k + (int64_t)ti.r0 * a.k_stride + kvh * D;
+      // two blocks of 64 rows; rows behind the end repeat the last one
+      dma_block<D, 64>(kbase, a.k_stride, k0, len - 1, wave, lds_addr(&lds.k[0]));
+      if (k0 + 64 < len) dma_block<D, 64>(kbase, a.k_stride, k0 + 64, len - 1, wave, lds_addr(&lds.k[0]) + 64 * D * 2);
+    }
+    request(0);
+    u32x4 kb4[D == 64 ? NT : 1], vb[NT];
+    {
+      const int64_t tok = ti.r0 + min(w0 + ln, len - 1);
+      const uint16_t* kp = a.k + tok * a.k_stride + kvh * D + 8 * g;
+      const uint16_t* vp = a.v + tok * a.v_stride + kvh * D + 8 * g;
+#pragma unroll
+      for (int t = 0; t < NT; t++) {
+        vb[t] = *reinterpret_cast<const u32x4*>(vp + 16 * t);
+        if (D == 64) kb4[t] = *reinterpret_cast<const u32x4*>(kp + 16 * t);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; t++) {
+        asm volatile("" ::"v"(vb[t]));
+        if (D == 64) asm volatile("" ::"v"(kb4[t]));
+      }
+    }
+    f32x16 dk[NC], dv[NC];
+#pragma unroll
+    for (int cb = 0; cb < NC; cb++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) dk[cb][r] = dv[cb][r] = 0.f;
+    const uint16_t* myk = &lds.k[0] + (wave >> 1) * (64 * D);
+
+    int stage = 0, qt = 0;
+    for (int i = 0; i < n; i++) {
+      wait_vmem<0>();
+      __syncthreads();
+      if (i + 1 < n) request(1 - stage);
+      const int q0 = (qt0 + qt) * kCausalQueries;
+      if (++qt == nq) qt = 0;
+      if (w0 < len && q0 >= w0) {
+        const auto& st = lds.ring[stage];
+        f32x16 s, dp;
+#pragma unroll
+        for (int r = 0; r < 16; r++) s[r] = dp[r] = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+          const u32x4 kk = D == 64 ? kb4[D == 64 ? t : 0] : read_rows<D, 64>(rr, myk, wave & 1, t);
+          s = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.q, 0, t), kk, s);
+          dp = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.g, 0, t), vb[t], dp);
+        }
+        float p[16], ds[16];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const f32x4 l4 = *reinterpret_cast<const f32x4*>(&st.stat[wave][8 * j + 4 * g]);
+          const f32x4 d4 = *reinterpret_cast<const f32x4*>(&st.stat[wave][32 + 8 * j + 4 * g]);
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const int r = 4 * j + e;
+            p[r] = fast_exp2(__builtin_fmaf(s[r], c2, -l4[e]));
+            ds[r] = p[r] * (dp[r] + d4[e]);
+          }
+        }
+        if (q0 == w0) {  // the diagonal: queries ahead of the lane's key
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (8 * (r >> 2) + 4 * g + (r & 3) < ln) p[r] = ds[r] = 0.f;
+        }
+        const u32x4 pb[2] = {pack_half<T>(p, 0), pack_half<T>(p, 1)}, dsb[2] = {pack_half<T>(ds, 0), pack_half<T>(ds, 1)};
+#pragma unroll
+        for (int t2 = 0; t2 < 2; t2++)
+#pragma unroll
+          for (int cb = 0; cb < NC; cb++) {
+            dv[cb] = Op<T>::mfma(read_cols<D, kCausalQueries>(cr, st.g, t2, cb), pb[t2], dv[cb]);
+            dk[cb] = Op<T>::mfma(read_cols<D, kCausalQueries>(cr, st.q, t2, cb), dsb[t2], dk[cb]);
+          }
+      }
+      stage = 1 - stage;
+    }
+    __syncthreads();
+    if (w0 < len) {
+      uint16_t* scratch = &lds.ring[0].q[0] + 2048 * wave;
+      static_assert(sizeof(lds.ring) >= 4 * 4096, "scratch of four wavefronts");
+      const int64_t tok = ti.r0 + w0;
+#pragma unroll
+      for (int h = 0; h < D / 64; h++) {
+        const f32x16 x[2] = {dk[2 * h], dk[2 * h + 1]}, y[2] = {dv[2 * h], dv[2 * h + 1]};
+        store_rows32<T>(x, a.scale, scratch, a.dk, tok * a.dk_stride + kvh * D + 64 * h, a.dk_stride, len - w0);
+        store_rows32<T>(y, 1.f, scratch, a.dv, tok * a.dv_stride + kvh * D + 64 * h, a.dv_stride, len - w0);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+}  // namespace fmha

@@ -35,6 +35,7 @@ EXPORTS = ("fmha_varlen_workspace_size", "fmha_varlen_fwd", "fmha_varlen_bwd",
            "fmha_rope_frequencies", "fmha_qk_norm_rope_fwd", "fmha_qk_norm_rope_bwd",
            "fmha_qk_norm_rope_bwd_workspace_size", "fmha_cache_append",
            "fmha_cache_attention", "fmha_cache_attention_workspace_size",
+           "fmha_causal_fwd", "fmha_causal_bwd", "fmha_causal_workspace_size",
            "fmha_varlen_schedule_info", "fmha_last_error")
 
 
@@ -96,6 +97,17 @@ class AppendParams(ctypes.Structure):
                 ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
                 ("q_out_stride", ctypes.c_int64), ("gamma_q", ctypes.c_void_p), ("gamma_k", ctypes.c_void_p),
                 ("cu_seqlens", ctypes.c_void_p), ("rope", RopeArgs)]
+
+
+class CausalParams(ctypes.Structure):
+    """Mirror of fmha_causal_params_t."""
+    _fields_ = [("batch", ctypes.c_int32), ("total_tokens", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("max_seqlen", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("scale", ctypes.c_float),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("o_stride", ctypes.c_int64), ("do_stride", ctypes.c_int64), ("dq_stride", ctypes.c_int64),
+                ("dk_stride", ctypes.c_int64), ("dv_stride", ctypes.c_int64), ("cu_seqlens", ctypes.c_void_p),
+                ("cu_seqlens_host", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
 class FmhaError(RuntimeError):
@@ -177,6 +189,12 @@ def lib():
         L.fmha_cache_attention.argtypes = [cp, i32, i32, ctypes.c_float, vp, ctypes.c_int64, vp, vp, vp, ctypes.c_int64, vp, vp,
                                            ctypes.c_size_t, vp]
         L.fmha_cache_attention.restype = ctypes.c_int
+        L.fmha_causal_workspace_size.argtypes = [i32] * 6
+        L.fmha_causal_workspace_size.restype = ctypes.c_size_t
+        L.fmha_causal_fwd.argtypes = [ctypes.POINTER(CausalParams)] + [vp] * 6
+        L.fmha_causal_fwd.restype = ctypes.c_int
+        L.fmha_causal_bwd.argtypes = [ctypes.POINTER(CausalParams)] + [vp] * 10
+        L.fmha_causal_bwd.restype = ctypes.c_int
         L.fmha_varlen_schedule_info.argtypes = [ctypes.c_int32] * 3 + [ctypes.POINTER(ctypes.c_size_t)] * 2
         L.fmha_varlen_schedule_info.restype = ctypes.c_int32
         L.fmha_last_error.restype = ctypes.c_char_p
@@ -648,3 +666,65 @@ def fmha_cache_attention(q, k_cache, v_cache, block_table, seqlens, max_seqlen, 
                                       k_cache.data_ptr(), v_cache.data_ptr(), o.data_ptr(), _tok_stride(o), lse.data_ptr(),
                                       _opt_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
                                       _stream()))
+
+
+def fmha_causal_workspace_size(batch: int, total_tokens: int, heads: int, kv_heads: int, head_dim: int, need_bwd: bool) -> int:
+    return int(lib().fmha_causal_workspace_size(batch, total_tokens, heads, kv_heads, head_dim, int(need_bwd)))
+
+
+def alloc_causal_workspace(batch: int, total_tokens: int, heads: int, kv_heads: int, head_dim: int, need_bwd: bool, device="cuda"):
+    n = fmha_causal_workspace_size(batch, total_tokens, heads, kv_heads, head_dim, need_bwd)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def _causal_params(q, k, v, cu_seqlens, max_seqlen, scale, workspace, cu_seqlens_host, reuse_schedule):
+    p = CausalParams()
+    p.batch = cu_seqlens.numel() - 1
+    p.total_tokens, p.heads, p.head_dim = q.shape
+    p.kv_heads = k.shape[1]
+    assert k.shape == v.shape == (p.total_tokens, p.kv_heads, p.head_dim) and q.dtype == k.dtype == v.dtype
+    p.max_seqlen = int(max_seqlen)
+    p.dtype = _dtype_code(q)
+    p.flags = FMHA_FLAG_REUSE_SCHEDULE if reuse_schedule else 0
+    p.scale = float(scale)
+    p.cu_seqlens = _i32_ptr(cu_seqlens)
+    keep = None
+    if cu_seqlens_host is not None:
+        keep = cu_seqlens_host.to(dtype=torch.int32, device="cpu").contiguous()
+        assert keep.numel() == p.batch + 1
+        p.cu_seqlens_host = keep.data_ptr()
+    if workspace is not None:
+        p.workspace = workspace.data_ptr()
+        p.workspace_bytes = workspace.numel() * workspace.element_size()
+    p.q_stride, p.k_stride, p.v_stride = _tok_stride(q), _tok_stride(k), _tok_stride(v)
+    return p, keep
+
+
+def _check_lse(lse, q):
+    assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == q.shape[0] * q.shape[1]
+
+
+def fmha_causal_fwd(q, k, v, cu_seqlens, max_seqlen, scale, o, lse, workspace, *, cu_seqlens_host=None, reuse_schedule=False):
+    """Causal attention over packed sequences: q, o [T, heads, D], k, v [T, kv_heads, D], lse [heads, T] fp32; fills o
+    and lse.  D is 64 or 128, kv_heads divides heads."""
+    p, keep = _causal_params(q, k, v, cu_seqlens, max_seqlen, scale, workspace, cu_seqlens_host, reuse_schedule)
+    _same_kind(q, o)
+    _check_lse(lse, q)
+    p.o_stride = _tok_stride(o)
+    _check(lib().fmha_causal_fwd(ctypes.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+                                 _stream()))
+    del keep
+
+
+def fmha_causal_bwd(q, k, v, o, d_o, lse, cu_seqlens, max_seqlen, scale, dq, dk, dv, workspace, *, cu_seqlens_host=None,
+                    reuse_schedule=False):
+    """Backward of fmha_causal_fwd; fills dq, dk, dv (dk, dv summed over the query heads that share them)."""
+    p, keep = _causal_params(q, k, v, cu_seqlens, max_seqlen, scale, workspace, cu_seqlens_host, reuse_schedule)
+    _same_kind(q, o, d_o, dq)
+    _same_kind(k, dk, dv)
+    _check_lse(lse, q)
+    p.o_stride, p.do_stride = _tok_stride(o), _tok_stride(d_o)
+    p.dq_stride, p.dk_stride, p.dv_stride = _tok_stride(dq), _tok_stride(dk), _tok_stride(dv)
+    _check(lib().fmha_causal_bwd(ctypes.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), d_o.data_ptr(),
+                                 lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _stream()))
+    del keep

@@ -33,7 +33,7 @@ def layout_rows(tmp_path, structs):
 def test_struct_layouts_against_the_c_compiler(tmp_path):
     from paper_2208_08124_amd import fmha
     structs = [("fmha_rope_t", fmha.RopeArgs), ("fmha_qk_params_t", fmha.QkParams), ("fmha_cache_t", fmha.Cache),
-               ("fmha_append_params_t", fmha.AppendParams)]
+               ("fmha_append_params_t", fmha.AppendParams), ("fmha_causal_params_t", fmha.CausalParams)]
     for (name, mirror), row in zip(structs, layout_rows(tmp_path, structs)):
         assert row == [ctypes.sizeof(mirror)] + [getattr(mirror, f[0]).offset for f in mirror._fields_], name
 
@@ -172,3 +172,46 @@ def test_cache_attention_refusals():
     f = fmha.fmha_cache_attention_workspace_size
     assert f(2, 4, 3, 64, 100) == 0 and f(2, 4, 2, 96, 100) == 0 and f(2, 4, 2, 64, -1) == 0
     assert f(2, 4, 2, 64, 100) == 0 and f(2, 4, 2, 64, 100000) > 0  # one workgroup each, and several
+
+
+def causal(fmha, **over):
+    p = fmha.CausalParams(batch=2, total_tokens=16, heads=4, kv_heads=2, head_dim=64, max_seqlen=8, dtype=0, scale=0.125, cu_seqlens=P,
+                          workspace=P, workspace_bytes=1 << 20)
+    keep = None
+    for n, v in over.items():
+        if n == "cu_host":
+            keep = np.asarray(v, dtype=np.int32)
+            n, v = "cu_seqlens_host", keep.ctypes.data
+        setattr(p, n, v)
+    return p, keep
+
+
+def test_causal_refusals():
+    from paper_2208_08124_amd import fmha
+    lib, (INV, UNS, WS) = fmha.lib(), (fmha.FMHA_ERR_INVALID_ARG, fmha.FMHA_ERR_UNSUPPORTED, fmha.FMHA_ERR_WORKSPACE)
+    bad = [(dict(head_dim=96), UNS, "head_dim"), (dict(dtype=2), UNS, "dtype"), (dict(batch=-1), INV, "batch"), (dict(total_tokens=-1), INV, "total"),
+           (dict(heads=0), INV, "heads"), (dict(kv_heads=3), INV, "kv_heads"), (dict(kv_heads=0), INV, "kv_heads"), (dict(kv_heads=-2), INV, "kv_heads"),
+           (dict(flags=2), INV, "flags"), (dict(scale=float("nan")), INV, "scale"), (dict(cu_seqlens=None), INV, "cu_seqlens"),
+           (dict(cu_seqlens=P + 2), INV, "aligned"), (dict(total_tokens=2 ** 31 - 1, heads=65536, kv_heads=1), INV, "tiles"),
+           (dict(cu_host=[1, 8, 16]), INV, "expected 0"), (dict(cu_host=[0, 8, 7]), INV, "decreases"), (dict(cu_host=[0, 8, 17]), INV, "max_seqlen"),
+           (dict(cu_host=[0, 8, 16], total_tokens=15), INV, "exceeds"), (dict(workspace=None), WS, "null"), (dict(workspace=P + 16), WS, "aligned"),
+           (dict(workspace_bytes=100), WS, "needed"), (dict(q_stride=64), INV, "q_stride"), (dict(k_stride=132), INV, "k_stride"),
+           (dict(v_stride=(1 << 24) + 8), INV, "v_stride"), (dict(o_stride=8), INV, "o_stride")]
+    for over, code, frag in bad:
+        p, keep = causal(fmha, **over)
+        for rc in (lib.fmha_causal_fwd(ctypes.byref(p), *[P] * 5, None), lib.fmha_causal_bwd(ctypes.byref(p), *[P] * 9, None)):
+            assert rc == code and frag in fmha.last_error(), (over, rc, fmha.last_error())
+    p, _ = causal(fmha)
+    assert lib.fmha_causal_fwd(None, *[P] * 5, None) == INV
+    for i in range(5):
+        assert lib.fmha_causal_fwd(ctypes.byref(p), *[None if i == j else P for j in range(5)], None) == INV, i
+    for i in range(9):
+        assert lib.fmha_causal_bwd(ctypes.byref(p), *[P + 2 if i == j else P for j in range(9)], None) == INV, i
+    for stride in ("do_stride", "dq_stride", "dk_stride", "dv_stride"):
+        p, _ = causal(fmha, **{stride: 100})
+        assert lib.fmha_causal_bwd(ctypes.byref(p), *[P] * 9, None) == INV and stride in fmha.last_error()
+    p, _ = causal(fmha, total_tokens=0)
+    assert lib.fmha_causal_fwd(ctypes.byref(p), *[None] * 5, None) == 0 and lib.fmha_causal_bwd(ctypes.byref(p), *[None] * 9, None) == 0
+    f = fmha.fmha_causal_workspace_size
+    assert f(-1, 10, 2, 1, 64, True) == 0 and f(1, 10, 3, 2, 64, True) == 0 and f(1, 10, 2, 1, 80, True) == 0
+    assert 0 < f(1, 10, 2, 1, 64, False) < f(1, 10, 2, 1, 64, True) <= f(100, 10, 2, 1, 64, True) <= f(100, 10, 2, 2, 128, True)
