@@ -13,21 +13,32 @@ using fmha_host::fail;
 using fmha_host::misaligned;
 
 struct Split {
-  int32_t chunk, splits;
+  int32_t chunk, splits, waves;
 };
 
-// Keys of a workgroup, and how many workgroups that makes of a sequence of `keys` keys.
-Split split_of(int32_t batch, int32_t heads, int32_t kv_heads, int64_t keys) {
-  const int64_t tiles = (heads / kv_heads + 15) / 16, items = batch * kv_heads * tiles;
-  int64_t parts = (2048 + items - 1) / (items > 0 ? items : 1);
+// Keys of a workgroup, how many workgroups that makes of a sequence of `keys` keys, and their wavefronts.  Times in us, of
+// calls in a graph, bf16, pages of 16.
+//  - Splitting costs a second launch (3 us and more), so short contexts are left whole, and where there are few
+//    (sequence, key head) items their workgroups have eight wavefronts: 4 x 12 heads of 64, 512 keys 8.2 split, 6.4 whole, 768
+//    8.1 / 7.8, 1024 8.4 / 9.2; 4 x 8 heads of 128, 512 9.8 / 9.4, 768 9.9 / 12.8.
+//  - Items that nearly fill the chip by themselves gain little by being split: 16 x 12 heads of 64, 1024 keys 14.6 / 11.9, 2048 23.4 /
+//    19.8; 16 x 8 heads of 128, 1024 17.9 / 17.5, 2048 28.4 / 28.3.
+//  - Few items are split so that the chip is filled once: 2 x 8 heads of 128, 131 072 keys, 201 for 512 workgroups, 206 for 1024,
+//    215 for 2048 (whose join reads more); more items, whose lengths may differ much, into pieces that even out.
+Split split_of(int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int64_t keys) {
+  const int64_t tiles = (heads / kv_heads + 15) / 16, items = (int64_t)batch * kv_heads * tiles;
+  const int whole = head_dim == 64 ? 768 : 512;
+  if (keys <= whole || (items >= 128 && items <= 256 && keys <= 4 * whole))
+    return Split{(int32_t)keys, 1, items <= 256 && keys > 128 ? 8 : 4};
+  const int64_t target = items < 64 ? 512 : 2048;
+  int64_t parts = (target + items - 1) / (items > 0 ? items : 1);
   const int64_t most = (keys + 255) / 256;
   if (parts > most) parts = most;
   if (parts < 1) parts = 1;
   int64_t chunk = (keys + parts - 1) / parts;
   chunk = (chunk + fmha::kCacheStep - 1) / fmha::kCacheStep * fmha::kCacheStep;
-  if (chunk < fmha::kCacheStep) chunk = fmha::kCacheStep;
   parts = (keys + chunk - 1) / chunk;
-  return Split{(int32_t)chunk, (int32_t)(parts < 1 ? 1 : parts)};
+  return Split{(int32_t)chunk, (int32_t)parts, 4};
 }
 
 size_t bytes_of(const Split& s, int32_t batch, int32_t heads, int32_t head_dim) {
@@ -37,13 +48,16 @@ size_t bytes_of(const Split& s, int32_t batch, int32_t heads, int32_t head_dim) 
 template <typename T, int D>
 int launch(const fmha::CacheArgs& a, hipStream_t st) {
   const int64_t grid = (int64_t)a.splits * a.batch * a.kv_heads * a.tiles;
-  if (grid > 0x7fffffff) return fail(FMHA_ERR_INVALID_ARG, "%lld workgroups: too many", (long long)grid);
-  fmha::cache_attention_kernel<T, D><<<(unsigned)grid, fmha::kCacheThreads, 0, st>>>(a);
+  if (grid > 0x7fffffff || (int64_t)a.batch * a.heads > 0x7fffffff)
+    return fail(FMHA_ERR_INVALID_ARG, "batch=%d, heads=%d: more than 2^31 workgroups", a.batch, a.heads);
+  if (a.waves == 8)
+    fmha::cache_attention_kernel<T, D, 8><<<(unsigned)grid, 512, 0, st>>>(a);
+  else
+    fmha::cache_attention_kernel<T, D, 4><<<(unsigned)grid, 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "cache attention launch failed: %s", hipGetErrorString(e));
   if (a.splits == 1) return FMHA_OK;
-  const int64_t rows = (int64_t)a.batch * a.heads, per = fmha::kCacheThreads / 64;
-  fmha::cache_join_kernel<T, D><<<(unsigned)((rows + per - 1) / per), fmha::kCacheThreads, 0, st>>>(a);
+  fmha::cache_join_kernel<T, D><<<(unsigned)(a.batch * a.heads), fmha::kCacheThreads, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "cache attention join launch failed: %s", hipGetErrorString(e));
   return FMHA_OK;
@@ -55,7 +69,7 @@ extern "C" {
 
 size_t fmha_cache_attention_workspace_size(int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_seqlen) {
   if (batch <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || (head_dim != 64 && head_dim != 128) || max_seqlen < 0) return 0;
-  return bytes_of(split_of(batch, heads, kv_heads, max_seqlen), batch, heads, head_dim);
+  return bytes_of(split_of(batch, heads, kv_heads, head_dim, max_seqlen), batch, heads, head_dim);
 }
 
 int fmha_cache_attention(const fmha_cache_t* c, int32_t heads, int32_t max_seqlen, float scale, const void* q, int64_t q_stride,
@@ -78,7 +92,7 @@ int fmha_cache_attention(const fmha_cache_t* c, int32_t heads, int32_t max_seqle
     return rc;
   int64_t keys = max_seqlen > 0 ? max_seqlen : (int64_t)c->max_pages * c->page_size;
   if (keys > 0x7fffffff) keys = 0x7fffffff;
-  const Split s = split_of(c->batch, heads, c->kv_heads, keys);
+  const Split s = split_of(c->batch, heads, c->kv_heads, c->head_dim, keys);
   const size_t need = bytes_of(s, c->batch, heads, c->head_dim);
   if (need) {
     if (!workspace) return fail(FMHA_ERR_WORKSPACE, "workspace is null (%zu bytes needed)", need);
@@ -102,6 +116,7 @@ int fmha_cache_attention(const fmha_cache_t* c, int32_t heads, int32_t max_seqle
   a.max_pages = c->max_pages;
   a.chunk = s.chunk;
   a.splits = s.splits;
+  a.waves = s.waves;
   a.scale = scale;
   a.part_o = static_cast<float*>(workspace);
   a.part_lse = a.part_o + (size_t)s.splits * (size_t)c->batch * (size_t)heads * (size_t)c->head_dim;

@@ -17,9 +17,9 @@
 
 namespace fmha {
 
-constexpr int kCacheThreads = 256, kCacheWaves = 4;
-constexpr int kCacheBlock = 32;                         // keys a wavefront takes at a time
-constexpr int kCacheStep = kCacheBlock * kCacheWaves;   // chunks are multiples of it
+constexpr int kCacheThreads = 256;  // of the join
+constexpr int kCacheBlock = 32;     // keys a wavefront takes at a time
+constexpr int kCacheStep = 8 * kCacheBlock;  // chunks are multiples of it
 
 struct CacheArgs {
   const uint16_t *q, *k, *v;
@@ -29,6 +29,7 @@ struct CacheArgs {
   int64_t q_stride, o_stride, page_stride;
   int32_t batch, heads, kv_heads, group, tiles;  // tiles of sixteen heads in a group
   int32_t page_shift, num_pages, max_pages;
+  int32_t waves;          // of a workgroup
   int32_t chunk, splits;  // keys of a workgroup; the last one takes what is left
   float scale;
   float* part_o;    // [splits][batch][heads][head_dim], where there are several
@@ -96,14 +97,16 @@ __device__ __forceinline__ void cache_request(CacheBlock<D>& blk, const CacheArg
   }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(kCacheThreads, D == 64 ? 3 : 2) void cache_attention_kernel(const CacheArgs a) {
+// W: wavefronts, four or (for few sequences that are not worth splitting over workgroups) eight.
+template <typename T, int D, int W>
+__global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void cache_attention_kernel(const CacheArgs a) {
+  constexpr int kThreads = 64 * W, kStep = W * kCacheBlock;
   constexpr int kOutRow = D + 4;  // floats; (16 lanes write 16 rows at a time)
   __shared__ __align__(16) union {
-    uint16_t v[kCacheWaves][D / 64][kCacheBlock * 64];
-    float o[kCacheWaves][16][kOutRow];
+    uint16_t v[W][D / 64][kCacheBlock * 64];
+    float o[W][16][kOutRow];
   } lds;
-  __shared__ float stat[2][kCacheWaves][16];  // maximum (log2 units) and sum
+  __shared__ float stat[2][W][16];  // maximum (log2 units) and sum
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, c = lane >> 4;
   int idx = blockIdx.x;
@@ -187,12 +190,12 @@ __global__ __launch_bounds__(kCacheThreads, D == 64 ? 3 : 2) void cache_attentio
   if (key0 < end) {
     CacheBlock<D> cur, next;
     const int first = cache_page(a, row, key0, end);
-    int page = cache_page(a, row, key0 + kCacheStep, end);
+    int page = cache_page(a, row, key0 + kStep, end);
     cache_request(cur, a, first, key0, hk);
-    for (; key0 < end; key0 += kCacheStep) {
-      const int page2 = cache_page(a, row, key0 + 2 * kCacheStep, end);
-      const bool more = key0 + kCacheStep < end;
-      if (more) cache_request(next, a, page, key0 + kCacheStep, hk);
+    for (; key0 < end; key0 += kStep) {
+      const int page2 = cache_page(a, row, key0 + 2 * kStep, end);
+      const bool more = key0 + kStep < end;
+      if (more) cache_request(next, a, page, key0 + kStep, hk);
       work(cur);
       cur = next;
       page = page2;
@@ -210,15 +213,15 @@ __global__ __launch_bounds__(kCacheThreads, D == 64 ? 3 : 2) void cache_attentio
 #pragma unroll
   for (int dt = 0; dt < D / 16; dt++) *reinterpret_cast<f32x4*>(&lds.o[wave][col][16 * dt + 4 * c]) = o[dt];
   __syncthreads();
-  for (int i = threadIdx.x; i < n_heads * (D / 4); i += kCacheThreads) {
+  for (int i = threadIdx.x; i < n_heads * (D / 4); i += kThreads) {
     const int h = i / (D / 4), x = 4 * (i % (D / 4));
     float top = -INFINITY, total = 0.f;
 #pragma unroll
-    for (int w = 0; w < kCacheWaves; w++) top = fmaxf(top, stat[0][w][h]);
+    for (int w = 0; w < W; w++) top = fmaxf(top, stat[0][w][h]);
     const float base = top == -INFINITY ? 0.f : top;
     f32x4 r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kCacheWaves; w++) {
+    for (int w = 0; w < W; w++) {
       const float share = fast_exp2(stat[0][w][h] - base);
       total += share * stat[1][w][h];
       r += share * *reinterpret_cast<const f32x4*>(&lds.o[w][h][x]);
@@ -238,36 +241,70 @@ __global__ __launch_bounds__(kCacheThreads, D == 64 ? 3 : 2) void cache_attentio
   }
 }
 
-// o and lse of a (sequence, head) from its parts, in the parts' order.  One wavefront each, D / 64 channels a lane.
+// o and lse of a (sequence, head) from its parts: a workgroup each, whose wavefronts take every fourth part and
+// are added up in order.  The weights are formed first, a part to a lane, so that the rows come in without waiting for them.
+constexpr int kJoinParts = 256;  // parts whose weights stand in LDS at a time
 template <typename T, int D>
 __global__ __launch_bounds__(kCacheThreads) void cache_join_kernel(const CacheArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * (kCacheThreads / 64) + (threadIdx.x >> 6), all = (int64_t)a.batch * a.heads;
-  if (at >= all) return;
+  constexpr int W = kCacheThreads / 64;
+  __shared__ float share[kJoinParts], tops[W];
+  __shared__ __align__(16) float rows[W][D];
+  __shared__ float sums[W];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t at = blockIdx.x, all = (int64_t)a.batch * a.heads;
   const int b = (int)(at / a.heads), h = (int)(at - (int64_t)b * a.heads);
   const int n = cache_keys(a, b);
   const int parts = max(1, min(a.splits, (n + a.chunk - 1) / a.chunk));
   float top = -INFINITY;
-  for (int s = lane; s < parts; s += 64) top = fmaxf(top, a.part_lse[s * all + at]);
+  for (int s = tid; s < parts; s += kCacheThreads) top = fmaxf(top, a.part_lse[s * all + at]);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < W; w++) top = fmaxf(top, tops[w]);
   const float base = top == -INFINITY ? 0.f : top;
   float x[D / 64] = {}, total = 0.f;
-#pragma unroll 8
-  for (int s = 0; s < parts; s++) {
-    const float share = fast_exp2(a.part_lse[s * all + at] - base);
-    const float* src = a.part_o + (s * all + at) * D + lane * (D / 64);
-    total += share;
+  for (int s0 = 0; s0 < parts; s0 += kJoinParts) {
+    __syncthreads();
+    for (int s = tid; s < kJoinParts; s += kCacheThreads)
+      share[s] = s0 + s < parts ? fast_exp2(a.part_lse[(s0 + s) * all + at] - base) : 0.f;
+    __syncthreads();
+    const int upto = min(kJoinParts, parts - s0);
+    for (int s = wave; s < upto; s += 16 * W) {
+      float y[16][D / 64];
 #pragma unroll
-    for (int i = 0; i < D / 64; i++) x[i] += share * src[i];
+      for (int i = 0; i < 16; i++) {
+        const float* src = a.part_o + ((s0 + min(s + i * W, upto - 1)) * all + at) * D + lane * (D / 64);
+#pragma unroll
+        for (int e = 0; e < D / 64; e++) y[i][e] = src[e];
+      }
+#pragma unroll
+      for (int i = 0; i < 16; i++) {
+        if (s + i * W >= upto) break;
+        const float f = share[s + i * W];
+        total += f;
+#pragma unroll
+        for (int e = 0; e < D / 64; e++) x[e] += f * y[i][e];
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < D / 64; e++) rows[wave][lane * (D / 64) + e] = x[e];
+  if (lane == 0) sums[wave] = total;
+  __syncthreads();
+  if (tid >= D / 2) return;
+  float r0 = 0.f, r1 = 0.f;
+  total = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; w++) {
+    total += sums[w];
+    r0 += rows[w][2 * tid];
+    r1 += rows[w][2 * tid + 1];
   }
   const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
-  uint16_t* out = a.o + b * a.o_stride + (int64_t)h * D + lane * (D / 64);
-  if (D == 128)
-    *reinterpret_cast<uint32_t*>(out) = Op<T>::pack2(x[0] * inv, x[D / 64 - 1] * inv);
-  else
-    *out = (uint16_t)Op<T>::pack2(x[0] * inv, 0.f);
-  if (lane == 0) a.lse[at] = top == -INFINITY ? top : (top + __log2f(total)) * kLn2;
+  *reinterpret_cast<uint32_t*>(a.o + b * a.o_stride + (int64_t)h * D + 2 * tid) = Op<T>::pack2(r0 * inv, r1 * inv);
+  if (tid == 0) a.lse[at] = top == -INFINITY ? top : (top + __log2f(total)) * kLn2;
 }
 
 }  // namespace fmha

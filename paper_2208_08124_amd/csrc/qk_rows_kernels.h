@@ -277,7 +277,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_kernel(const QkRows a) {
 // workgroups, always in the same order.  partial: [workgroups][2][dim].
 template <typename T, bool INTER>
 __global__ __launch_bounds__(kQkThreads) void qk_rows_bwd_kernel(const QkRows a) {
-  __shared__ float sums[kQkThreads / 64][2][256];
+  __shared__ float sums[kQkThreads / 64][2][256];  // (first gamma: [0][0] of the queries, [0][1] of the keys)
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int slots = 64 / a.lp2, tpw = slots / a.gs;
   const int present = qk_present(a);
@@ -286,58 +286,80 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_bwd_kernel(const QkRows a)
   const QkPieces pc = QkPieces::of<INTER>(c, a.lph, a.rot);
   const int heads = a.nq + a.nk;
   const int groups = (present + tpw - 1) / tpw;
+  for (int i = threadIdx.x; i < a.dim; i += kQkThreads) {
+    sums[0][0][i] = a.gamma_q ? a.gamma_q[i] : 1.f;
+    sums[0][1][i] = a.gamma_k ? a.gamma_k[i] : 1.f;
+  }
+  __syncthreads();
+  struct Raw {
+    u32x4 g1, g2, x1, x2;
+  };
+  // (an empty place, or a lane that its head is padded with, works on zeros)
+  auto fetch = [&](Raw& r, int tok, int h) {
+    r.g1 = r.g2 = r.x1 = r.x2 = u32x4{0u, 0u, 0u, 0u};
+    if (!on || h >= heads || tok >= present) return;
+    const bool is_q = h < a.nq;
+    const int64_t col = (int64_t)(is_q ? h : h - a.nq) * a.dim;
+    const uint16_t* dy = is_q ? a.dyq + tok * a.qo_stride + col : a.dyk + tok * a.ko_stride + col;
+    r.g1 = *reinterpret_cast<const u32x4*>(dy + 8 * pc.one);
+    r.g2 = *reinterpret_cast<const u32x4*>(dy + 8 * pc.two);
+    if (is_q ? a.gamma_q : a.gamma_k) {
+      const uint16_t* xs = is_q ? a.q + tok * a.q_stride + col : a.k + tok * a.k_stride + col;
+      r.x1 = *reinterpret_cast<const u32x4*>(xs + 8 * pc.one);
+      r.x2 = *reinterpret_cast<const u32x4*>(xs + 8 * pc.two);
+    }
+  };
   float sum_q[16] = {}, sum_k[16] = {};
   for (int group = blockIdx.x * (kQkThreads / 64) + w; group < groups; group += gridDim.x * (kQkThreads / 64)) {
     const int tok0 = __builtin_amdgcn_readfirstlane(group * tpw), tok = tok0 + mine;
+    Raw cur;
+    fetch(cur, tok, slot % a.gs);
     int seq;
     const int pos = a.rot ? qk_position<false>(a, tok0, tpw, mine, present, seq) : 0;
-    if (tok < present) {
-      float cs[8], sn[8];
-      if (on) qk_angles<INTER>(cs, sn, pc, a.inv_freq, pos, a.magnitude);
-      for (int h = slot % a.gs; h < heads; h += a.gs) {
-        const bool is_q = h < a.nq;
-        const int64_t col = (int64_t)(is_q ? h : h - a.nq) * a.dim;
-        const uint16_t* dy = is_q ? a.dyq + tok * a.qo_stride + col : a.dyk + tok * a.ko_stride + col;
-        uint16_t* dx = is_q ? a.dq + tok * a.dq_stride + col : a.dk + tok * a.dk_stride + col;
-        const float* gamma = is_q ? a.gamma_q : a.gamma_k;
-        float g[16] = {}, x[16] = {};
-        if (on) {
-          qk_unpack<T>(g, *reinterpret_cast<const u32x4*>(dy + 8 * pc.one), *reinterpret_cast<const u32x4*>(dy + 8 * pc.two));
-          if (gamma) {
-            const uint16_t* xs = is_q ? a.q + tok * a.q_stride + col : a.k + tok * a.k_stride + col;
-            qk_unpack<T>(x, *reinterpret_cast<const u32x4*>(xs + 8 * pc.one), *reinterpret_cast<const u32x4*>(xs + 8 * pc.two));
-          }
-          qk_turn<INTER, true>(g, cs, sn, pc);
-        }
-        if (gamma) {
-          float wt[16] = {}, ss = 0.f, dot = 0.f;
-          if (on) qk_gamma(wt, gamma, pc);
+    if (tok >= present) continue;  // (whole heads)
+    float cs[8], sn[8];
+    if (on) qk_angles<INTER>(cs, sn, pc, a.inv_freq, pos, a.magnitude);
+    for (int h = slot % a.gs; h < heads; h += a.gs) {
+      Raw next;
+      fetch(next, tok, h + a.gs);  // the next head's rows, ahead of this one's work
+      const bool is_q = h < a.nq;
+      const bool normed = is_q ? a.gamma_q : a.gamma_k;
+      float g[16];
+      qk_unpack<T>(g, cur.g1, cur.g2);
+      if (on) qk_turn<INTER, true>(g, cs, sn, pc);
+      if (normed) {
+        float x[16], wt[16] = {}, ss = 0.f, dot = 0.f;
+        qk_unpack<T>(x, cur.x1, cur.x2);
+        if (on) qk_gamma(wt, sums[0][is_q ? 0 : 1], pc);
 #pragma unroll
-          for (int j = 0; j < 16; j++) {
-            ss += x[j] * x[j];
-            dot += g[j] * wt[j] * x[j];
-          }
-          ss = qk_head_sum(ss, a.lp2);
-          dot = qk_head_sum(dot, a.lp2);
-          const float rstd = 1.f / sqrtf(ss / (float)a.dim + a.eps);
-          const float m = dot * rstd / (float)a.dim;  // mean(g gamma xh)
-#pragma unroll
-          for (int j = 0; j < 16; j++) {
-            const float xh = x[j] * rstd;
-            if (is_q)
-              sum_q[j] += g[j] * xh;
-            else
-              sum_k[j] += g[j] * xh;
-            g[j] = rstd * (g[j] * wt[j] - xh * m);
-          }
+        for (int j = 0; j < 16; j++) {
+          wt[j] *= g[j];
+          ss += x[j] * x[j];
+          dot += wt[j] * x[j];
         }
-        if (on) {
-          u32x4 w1, w2;
-          qk_pack<T>(w1, w2, g);
-          *reinterpret_cast<u32x4*>(dx + 8 * pc.one) = w1;
-          *reinterpret_cast<u32x4*>(dx + 8 * pc.two) = w2;
+        ss = qk_head_sum(ss, a.lp2);
+        dot = qk_head_sum(dot, a.lp2);
+        const float rstd = 1.f / sqrtf(ss / (float)a.dim + a.eps);
+        const float m = dot * rstd / (float)a.dim;  // mean(g gamma xh)
+#pragma unroll
+        for (int j = 0; j < 16; j++) {
+          const float xh = x[j] * rstd;
+          if (is_q)
+            sum_q[j] += g[j] * xh;
+          else
+            sum_k[j] += g[j] * xh;
+          g[j] = rstd * (wt[j] - xh * m);
         }
       }
+      if (on) {
+        const int64_t col = (int64_t)(is_q ? h : h - a.nq) * a.dim;
+        uint16_t* dx = is_q ? a.dq + tok * a.dq_stride + col : a.dk + tok * a.dk_stride + col;
+        u32x4 w1, w2;
+        qk_pack<T>(w1, w2, g);
+        *reinterpret_cast<u32x4*>(dx + 8 * pc.one) = w1;
+        *reinterpret_cast<u32x4*>(dx + 8 * pc.two) = w2;
+      }
+      cur = next;
     }
   }
   if (!a.gamma_q && !a.gamma_k) return;
@@ -348,6 +370,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_bwd_kernel(const QkRows a)
       sum_k[j] += __shfl_xor(sum_k[j], m, 64);
     }
   }
+  __syncthreads();  // gamma is done with
   if (slot == 0 && on) {
 #pragma unroll
     for (int j = 0; j < 16; j++) {
@@ -373,8 +396,18 @@ __global__ __launch_bounds__(kQkGammaThreads) void qk_gamma_kernel(const float* 
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int col = blockIdx.x * 64 + lane;
   float s = 0.f;
-  if (col < 2 * dim)
-    for (int r = w; r < rows; r += 16) s += partial[(int64_t)r * 2 * dim + col];
+  if (col < 2 * dim) {
+    const float* src = partial + (int64_t)w * 2 * dim + col;
+    const int64_t step = (int64_t)16 * 2 * dim;
+    for (int r = w; r < rows; r += 16 * 16) {  // sixteen rows in flight: one after the other takes 27 us for 1024 rows of 256
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; i++) x[i] = r + 16 * i < rows ? src[i * step] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; i++) s += x[i];
+      src += 16 * step;
+    }
+  }
   sums[w][lane] = s;
   __syncthreads();
   if (w == 0 && col < 2 * dim) {

@@ -269,8 +269,15 @@ def _params(q, cu_seqlens, max_seqlen, scale, workspace, seqused, cu_seqlens_hos
     return p, keep
 
 
+# The current stream's handle, without the Stream object around it: 0.3 us a call in place of 2.8, of the 9 that
+# the smallest calls take.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    if _raw_stream is None:
+        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
 
 
 def _dropout(dropout):
@@ -503,12 +510,21 @@ def fmha_rope_frequencies(rotary_dim, base=10000.0, scaling="plain", factor=1.0,
     return out, float(m.value)
 
 
+def _here(*tensors):
+    """The current stream's handle; refuses tensors that are not on the current device, whose stream that is."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise FmhaError(FMHA_ERR_INVALID_ARG, f"a tensor is on {t.device}, the current device is cuda:{dev}")
+    return _stream() if _raw_stream is None else ctypes.c_void_p(_raw_stream(dev))
+
+
 def _rope(rope):
     """(inv_freq float64 device tensor, "half" | "interleaved", magnitude) or None -> fmha_rope_t"""
     if rope is None:
         return RopeArgs(0, 0, None, 1.0)
     inv_freq, layout, magnitude = rope
-    assert inv_freq.dtype == torch.float64 and inv_freq.is_cuda and inv_freq.is_contiguous()
+    assert inv_freq.dtype == torch.float64 and inv_freq.is_contiguous()
     if layout not in ROPE_LAYOUTS:
         raise FmhaError(FMHA_ERR_INVALID_ARG, f"layout {layout!r} is not one of {sorted(ROPE_LAYOUTS)}")
     return RopeArgs(2 * inv_freq.numel(), ROPE_LAYOUTS[layout], inv_freq.data_ptr(), float(magnitude))
@@ -517,7 +533,7 @@ def _rope(rope):
 def _i32_ptr(t, at_least=None):
     if t is None:
         return None
-    assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()
+    assert t.dtype == torch.int32 and t.is_contiguous()
     assert at_least is None or t.numel() >= at_least
     return t.data_ptr()
 
@@ -525,7 +541,7 @@ def _i32_ptr(t, at_least=None):
 def _gamma_ptr(g, dim):
     if g is None:
         return None
-    assert g.dtype == torch.float32 and g.is_cuda and g.is_contiguous() and g.numel() == dim
+    assert g.dtype == torch.float32 and g.is_contiguous() and g.numel() == dim
     return g.data_ptr()
 
 
@@ -535,7 +551,7 @@ def _opt_ptr(t):
 
 def _same_kind(like, *tensors):
     for t in tensors:
-        assert t is None or (t.dtype == like.dtype and t.is_cuda and t.shape == like.shape)
+        assert t is None or (t.dtype == like.dtype and t.shape == like.shape)
 
 
 def _qk_params(q, k, rope, gamma_q, gamma_k, eps, positions, cu_seqlens, n_rows):
@@ -569,8 +585,9 @@ def fmha_qk_norm_rope_fwd(q, k, q_out, k_out, *, rope=None, gamma_q=None, gamma_
     if k is not None:
         _same_kind(k, k_out)
         p.k_stride, p.k_out_stride = _tok_stride(k), _tok_stride(k_out)
+    stream = _here(q, k, q_out, k_out, gamma_q, gamma_k, positions, cu_seqlens, n_rows, None if rope is None else rope[0])
     _check(lib().fmha_qk_norm_rope_fwd(ctypes.byref(p), _opt_ptr(q), _opt_ptr(k), _opt_ptr(q_out), _opt_ptr(k_out),
-                                       _stream()))
+                                       stream))
 
 
 def fmha_qk_norm_rope_bwd_workspace_size(rows: int, q_heads: int, k_heads: int, head_dim: int) -> int:
@@ -595,22 +612,24 @@ def fmha_qk_norm_rope_bwd(dq_out, dk_out, q, k, dq, dk, dgamma_q, dgamma_k, work
         _same_kind(dk_out, dk, k)
         p.k_out_stride, p.dk_stride = _tok_stride(dk_out), _tok_stride(dk)
         p.k_stride = _tok_stride(k) if k is not None else 0
+    stream = _here(dq_out, dk_out, q, k, dq, dk, dgamma_q, dgamma_k, workspace, gamma_q, gamma_k, positions, cu_seqlens, n_rows,
+                   None if rope is None else rope[0])
     _check(lib().fmha_qk_norm_rope_bwd(ctypes.byref(p), _opt_ptr(dq_out), _opt_ptr(dk_out), _opt_ptr(q), _opt_ptr(k),
                                        _opt_ptr(dq), _opt_ptr(dk), _gamma_ptr(dgamma_q, p.head_dim),
                                        _gamma_ptr(dgamma_k, p.head_dim), _opt_ptr(workspace),
                                        0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                       _stream()))
+                                       stream))
 
 
 def _cache(k_cache, v_cache, block_table, seqlens):
     """k_cache, v_cache [num_pages, kv_heads, page_size, D], a page contiguous; block_table int32 [batch, max_pages];
     seqlens int32 [batch] -> fmha_cache_t"""
     ks, vs, shape = k_cache.stride(), v_cache.stride(), k_cache.shape
-    assert shape == v_cache.shape and len(shape) == 4 and k_cache.dtype == v_cache.dtype and k_cache.is_cuda and v_cache.is_cuda
+    assert shape == v_cache.shape and len(shape) == 4 and k_cache.dtype == v_cache.dtype
     assert ks == vs or shape[0] <= 1
     assert ks[1:] == vs[1:] == (shape[2] * shape[3], shape[3], 1), "a page is [kv_heads, page_size, D], contiguous"
-    assert block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous() and block_table.is_cuda
-    assert seqlens.dtype == torch.int32 and seqlens.is_contiguous() and seqlens.is_cuda and seqlens.numel() == block_table.shape[0]
+    assert block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous()
+    assert seqlens.dtype == torch.int32 and seqlens.is_contiguous() and seqlens.numel() == block_table.shape[0]
     c = Cache()
     c.batch, c.max_pages = block_table.shape
     c.num_pages, c.kv_heads, c.page_size, c.head_dim = shape
@@ -629,7 +648,8 @@ def fmha_cache_append(k, v, k_cache, v_cache, block_table, seqlens, *, cu_seqlen
     c = _cache(k_cache, v_cache, block_table, seqlens)
     p = AppendParams()
     p.rows = k.shape[0]
-    assert k.shape == v.shape and k.shape[1:] == (c.kv_heads, c.head_dim) and k.dtype == v.dtype == k_cache.dtype
+    assert k.shape[1:] == (c.kv_heads, c.head_dim) and k.dtype == k_cache.dtype
+    _same_kind(k, v)
     assert cu_seqlens is None or cu_seqlens.numel() == c.batch + 1
     p.eps = float(eps)
     p.k_stride, p.v_stride = _tok_stride(k), _tok_stride(v)
@@ -641,8 +661,10 @@ def fmha_cache_append(k, v, k_cache, v_cache, block_table, seqlens, *, cu_seqlen
     p.gamma_q, p.gamma_k = _gamma_ptr(gamma_q, c.head_dim), _gamma_ptr(gamma_k, c.head_dim)
     p.cu_seqlens = _i32_ptr(cu_seqlens)
     p.rope = _rope(rope)
+    stream = _here(k, v, k_cache, v_cache, block_table, seqlens, cu_seqlens, q, q_out, gamma_q, gamma_k,
+                   None if rope is None else rope[0])
     _check(lib().fmha_cache_append(ctypes.byref(c), ctypes.byref(p), _opt_ptr(q), k.data_ptr(), v.data_ptr(),
-                                   _opt_ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), _stream()))
+                                   _opt_ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), stream))
 
 
 def fmha_cache_attention_workspace_size(batch: int, heads: int, kv_heads: int, head_dim: int, max_seqlen: int) -> int:
@@ -662,10 +684,11 @@ def fmha_cache_attention(q, k_cache, v_cache, block_table, seqlens, max_seqlen, 
     assert q.shape[0] == c.batch and q.shape[2] == c.head_dim and q.dtype == k_cache.dtype
     _same_kind(q, o)
     assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == c.batch * q.shape[1]
+    stream = _here(q, k_cache, v_cache, block_table, seqlens, o, lse, workspace)
     _check(lib().fmha_cache_attention(ctypes.byref(c), q.shape[1], int(max_seqlen), float(scale), q.data_ptr(), _tok_stride(q),
                                       k_cache.data_ptr(), v_cache.data_ptr(), o.data_ptr(), _tok_stride(o), lse.data_ptr(),
                                       _opt_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                      _stream()))
+                                      stream))
 
 
 def fmha_causal_workspace_size(batch: int, total_tokens: int, heads: int, kv_heads: int, head_dim: int, need_bwd: bool) -> int:
@@ -682,7 +705,8 @@ def _causal_params(q, k, v, cu_seqlens, max_seqlen, scale, workspace, cu_seqlens
     p.batch = cu_seqlens.numel() - 1
     p.total_tokens, p.heads, p.head_dim = q.shape
     p.kv_heads = k.shape[1]
-    assert k.shape == v.shape == (p.total_tokens, p.kv_heads, p.head_dim) and q.dtype == k.dtype == v.dtype
+    assert k.shape == (p.total_tokens, p.kv_heads, p.head_dim) and q.dtype == k.dtype
+    _same_kind(k, v)
     p.max_seqlen = int(max_seqlen)
     p.dtype = _dtype_code(q)
     p.flags = FMHA_FLAG_REUSE_SCHEDULE if reuse_schedule else 0
@@ -711,8 +735,9 @@ def fmha_causal_fwd(q, k, v, cu_seqlens, max_seqlen, scale, o, lse, workspace, *
     _same_kind(q, o)
     _check_lse(lse, q)
     p.o_stride = _tok_stride(o)
+    stream = _here(q, k, v, cu_seqlens, o, lse, workspace)
     _check(lib().fmha_causal_fwd(ctypes.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
-                                 _stream()))
+                                 stream))
     del keep
 
 
@@ -725,6 +750,7 @@ def fmha_causal_bwd(q, k, v, o, d_o, lse, cu_seqlens, max_seqlen, scale, dq, dk,
     _check_lse(lse, q)
     p.o_stride, p.do_stride = _tok_stride(o), _tok_stride(d_o)
     p.dq_stride, p.dk_stride, p.dv_stride = _tok_stride(dq), _tok_stride(dk), _tok_stride(dv)
+    stream = _here(q, k, v, o, d_o, lse, cu_seqlens, dq, dk, dv, workspace)
     _check(lib().fmha_causal_bwd(ctypes.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), d_o.data_ptr(),
-                                 lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _stream()))
+                                 lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), stream))
     del keep
