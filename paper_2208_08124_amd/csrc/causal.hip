@@ -19,18 +19,46 @@ size_t round_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 // Tiles of 128 rows at most, for any lengths.
 int64_t tile_capacity(int64_t batch, int64_t total) { return total / fmha::kTileRows + batch; }
 
+// The dK/dV pass: its items are key tiles by key heads, of steps = group x (blocks of 32 queries from the diagonal on).
+// Where the longest item has much more than a workgroup's share of all steps (of 512 that run at a time), the chip would wait for
+// it, and items are cut into parts of at least 16 steps.  The share is estimated from below, by sequences that are all as long.
+// Cutting costs the parts' sums on their way through memory.  Backward, us, whole / cut (in how many), head size 128:
+//   1 x 16384, 16 / 2 heads    longest 4.0 shares   8000 / 5276 (4), 4399 (8), 3888 (16)
+//   6 x up to 4096, 32 / 8     1.9                  1488 / 1472 (3), 1430 (5)
+//   12 x up to 4000, 32 / 8    1.3                  2028 / 2216 (2)
+//   1 x 16384, 32 / 8          1.0                  7084 / 7265 (4)
+//   64 x 512, 16 / 4           1.0                   403 / 458 (2), 604 (4)
+constexpr int64_t kPartsMost = 16, kPartSteps = 16, kPartBytes = (int64_t)512 << 20;
+int64_t steps_of(int64_t len, int64_t group) { return (len + fmha::kCausalQueries - 1) / fmha::kCausalQueries * group; }
+int64_t parts_for(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, int64_t longest) {
+  if (batch <= 0 || total <= 0 || steps_of(longest, group) <= kPartSteps) return 1;
+  const double share = (double)kv_heads * (double)total * ((double)total / (double)batch) / (2. * fmha::kTileRows * fmha::kCausalQueries * 512.);
+  const double ratio = (double)longest / fmha::kCausalQueries / share;  // (the group counts on both sides)
+  if (ratio < 1.8) return 1;
+  const int64_t parts = ratio > kPartsMost / 4 ? kPartsMost : (int64_t)(4. * ratio + 0.5), most = (steps_of(longest, group) + kPartSteps - 1) / kPartSteps;
+  return parts < most ? parts : most;
+}
+
 struct Workspace {
-  size_t list, lse2, dsum, bytes_fwd, bytes_bwd;  // offsets (the number of tiles stands at 0), sizes
+  int64_t parts;  // of an item of the dK/dV pass at most
+  size_t by_sequence, by_cost, lse2, dsum, part_sums, bytes_fwd, bytes_bwd;  // offsets (the number of tiles stands at 0), sizes
 };
 
-Workspace carve(int64_t batch, int64_t total, int64_t heads) {
+Workspace carve(int64_t batch, int64_t total, int64_t heads, int64_t kv_heads, int64_t head_dim) {
   Workspace w;
-  w.list = kAlign;
-  w.bytes_fwd = round_up(w.list + sizeof(fmha::TileItem) * (size_t)tile_capacity(batch, total));
+  const size_t list = batch > fmha::kCausalSelf ? sizeof(fmha::TileItem) * (size_t)tile_capacity(batch, total) : 0;
+  w.by_sequence = kAlign;
+  w.by_cost = w.by_sequence + list;
+  w.bytes_fwd = round_up(w.by_cost + list);
   const size_t stat = round_up(sizeof(float) * ((size_t)total * (size_t)heads + 1));
   w.lse2 = w.bytes_fwd;
   w.dsum = w.lse2 + stat;
-  w.bytes_bwd = w.dsum + stat;
+  w.part_sums = w.dsum + stat;
+  const size_t one = (size_t)(tile_capacity(batch, total) * kv_heads) * 2 * fmha::kTileRows * (size_t)head_dim * sizeof(float);
+  w.parts = parts_for(batch, total, heads / kv_heads, kv_heads, total);
+  if ((size_t)w.parts * one > (size_t)kPartBytes) w.parts = (int64_t)((size_t)kPartBytes / one);
+  if (w.parts < 1) w.parts = 1;
+  w.bytes_bwd = w.part_sums + (w.parts > 1 ? (size_t)w.parts * one : 0);
   return w;
 }
 
@@ -42,6 +70,7 @@ int check_common(const fmha_causal_params_t* p, bool bwd, fmha::CausalArgs* a) {
   if (p->total_tokens < 0) return fail(FMHA_ERR_INVALID_ARG, "total_tokens=%d is negative", p->total_tokens);
   if (p->heads <= 0 || p->heads > 65536 || p->kv_heads <= 0 || p->heads % p->kv_heads)
     return fail(FMHA_ERR_INVALID_ARG, "heads=%d must be a positive multiple of kv_heads=%d (and at most 65536)", p->heads, p->kv_heads);
+  // (times sixteen parts at most, which only few tiles have)
   if (tile_capacity(p->batch, p->total_tokens) * p->heads > (int64_t)1 << 30)
     return fail(FMHA_ERR_INVALID_ARG, "total_tokens=%d, batch=%d, heads=%d: more than 2^30 tiles", p->total_tokens, p->batch, p->heads);
   if (p->flags & ~FMHA_FLAG_REUSE_SCHEDULE) return fail(FMHA_ERR_INVALID_ARG, "flags=%u: only FMHA_FLAG_REUSE_SCHEDULE is known here", p->flags);
@@ -58,7 +87,7 @@ int check_common(const fmha_causal_params_t* p, bool bwd, fmha::CausalArgs* a) {
     if (cu[p->batch] > p->total_tokens)
       return fail(FMHA_ERR_INVALID_ARG, "cu_seqlens_host[batch]=%d exceeds total_tokens=%d", cu[p->batch], p->total_tokens);
   }
-  const Workspace w = carve(p->batch, p->total_tokens, p->heads);
+  const Workspace w = carve(p->batch, p->total_tokens, p->heads, p->kv_heads, p->head_dim);
   const size_t need = bwd ? w.bytes_bwd : w.bytes_fwd;
   if (!p->workspace) return fail(FMHA_ERR_WORKSPACE, "workspace is null (%zu bytes needed)", need);
   if (misaligned(p->workspace, kAlign)) return fail(FMHA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
@@ -80,13 +109,19 @@ int check_common(const fmha_causal_params_t* p, bool bwd, fmha::CausalArgs* a) {
   a->kv_heads = p->kv_heads;
   a->group = p->heads / p->kv_heads;
   a->scale = p->scale;
-  if (p->batch > fmha::kCausalSelf) {
-    a->count = reinterpret_cast<int32_t*>(base);
-    a->list = reinterpret_cast<fmha::TileItem*>(base + w.list);
-  }
   if (bwd) {
     a->lse2 = reinterpret_cast<float*>(base + w.lse2);
     a->dsum = reinterpret_cast<float*>(base + w.dsum);
+    a->part_sums = reinterpret_cast<float*>(base + w.part_sums);
+    int64_t parts = w.parts;
+    const int64_t longest = p->max_seqlen > 0 && p->max_seqlen < p->total_tokens ? p->max_seqlen : p->total_tokens;
+    const int64_t steps = steps_of(longest, a->group);
+    const int64_t wanted = parts_for(p->batch, p->total_tokens, a->group, p->kv_heads, longest);
+    if (parts > wanted) parts = wanted;
+    a->chunk = (int32_t)((steps + parts - 1) / parts);
+    if (a->chunk < kPartSteps) a->chunk = kPartSteps;
+    a->chunk = (a->chunk + a->group - 1) / a->group * a->group;
+    a->parts = (int32_t)(steps <= a->chunk ? 1 : (steps + a->chunk - 1) / a->chunk);
   }
   return FMHA_OK;
 }
@@ -103,31 +138,59 @@ unsigned grid_of(const fmha_causal_params_t* p, int heads) {
   return (unsigned)(g < 1 ? 1 : g);
 }
 
+// Items up to which the tiles are taken by cost.  us, by sequence / by cost: 64 x 512 tokens, 16 / 4 heads of 128, backward
+// (1280 items of keys) 465 / 408; 8 x 4096, 32 / 32 heads of 128, forward (8192) 1160 / 1566.
+constexpr unsigned kByCost = 2048;
+
 int launch_list(const fmha_causal_params_t* p, const fmha::CausalArgs& a, hipStream_t st) {
-  if (!a.list || (p->flags & FMHA_FLAG_REUSE_SCHEDULE)) return FMHA_OK;
-  fmha::causal_list_kernel<<<1, fmha::kCausalListThreads, 0, st>>>(a, const_cast<int32_t*>(a.count), const_cast<fmha::TileItem*>(a.list),
+  if (p->batch <= fmha::kCausalSelf || (p->flags & FMHA_FLAG_REUSE_SCHEDULE)) return FMHA_OK;
+  const Workspace w = carve(p->batch, p->total_tokens, p->heads, p->kv_heads, p->head_dim);
+  char* base = static_cast<char*>(p->workspace);
+  fmha::causal_list_kernel<<<2, fmha::kCausalListThreads, 0, st>>>(a, reinterpret_cast<int32_t*>(base),
+                                                                   reinterpret_cast<fmha::TileItem*>(base + w.by_sequence),
+                                                                   reinterpret_cast<fmha::TileItem*>(base + w.by_cost),
                                                                    (int)tile_capacity(p->batch, p->total_tokens));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "tile list launch failed: %s", hipGetErrorString(e));
   return FMHA_OK;
 }
 
+// Workgroups for a pass over the tiles of `heads` heads, and the order in which it takes them.
+unsigned plan(const fmha_causal_params_t* p, int heads, fmha::CausalArgs* a) {
+  const unsigned grid = grid_of(p, heads);
+  a->by_cost = grid <= kByCost;
+  if (p->batch > fmha::kCausalSelf) {
+    const Workspace w = carve(p->batch, p->total_tokens, p->heads, p->kv_heads, p->head_dim);
+    char* base = static_cast<char*>(p->workspace);
+    a->count = reinterpret_cast<int32_t*>(base);
+    a->list = reinterpret_cast<fmha::TileItem*>(base + (a->by_cost ? w.by_cost : w.by_sequence));
+  }
+  return grid;
+}
+
 template <typename T, int D>
-int launch_fwd(const fmha_causal_params_t* p, const fmha::CausalArgs& a, hipStream_t st) {
-  fmha::causal_fwd_kernel<T, D><<<grid_of(p, a.heads), fmha::kThreads, 0, st>>>(a);
+int launch_fwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st) {
+  const unsigned grid = plan(p, a.heads, &a);
+  fmha::causal_fwd_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal forward launch failed: %s", hipGetErrorString(e));
   return FMHA_OK;
 }
 
 template <typename T, int D>
-int launch_bwd(const fmha_causal_params_t* p, const fmha::CausalArgs& a, hipStream_t st) {
-  fmha::causal_dq_kernel<T, D><<<grid_of(p, a.heads), fmha::kThreads, 0, st>>>(a);
+int launch_bwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st) {
+  unsigned grid = plan(p, a.heads, &a);
+  fmha::causal_dq_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal dQ launch failed: %s", hipGetErrorString(e));
-  fmha::causal_dkv_kernel<T, D><<<grid_of(p, a.kv_heads), fmha::kThreads, 0, st>>>(a);
+  grid = plan(p, a.kv_heads * a.parts, &a);
+  fmha::causal_dkv_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal dK/dV launch failed: %s", hipGetErrorString(e));
+  if (a.parts == 1) return FMHA_OK;
+  fmha::causal_dkv_join_kernel<T, D><<<grid / a.parts, fmha::kThreads, 0, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal dK/dV join launch failed: %s", hipGetErrorString(e));
   return FMHA_OK;
 }
 
@@ -141,7 +204,7 @@ extern "C" {
 size_t fmha_causal_workspace_size(int32_t batch, int32_t total_tokens, int32_t heads, int32_t kv_heads, int32_t head_dim,
                                   int32_t need_bwd) {
   if (batch < 0 || total_tokens < 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || (head_dim != 64 && head_dim != 128)) return 0;
-  const Workspace w = carve(batch, total_tokens, heads);
+  const Workspace w = carve(batch, total_tokens, heads, kv_heads, head_dim);
   return need_bwd ? w.bytes_bwd : w.bytes_fwd;
 }
 

@@ -3,7 +3,9 @@
 //              S^T = K Q^T,  dP^T = V dO^T,  P^T = exp(S^T - LSE),  dS^T = P^T o (dP^T - D),  dQ^T += K^T dS^T
 //   dK/dV pass per tile of 128 keys and key head: for every query head that shares it and every block of queries from the
 //              diagonal on  S = Q K^T,  dP = dO V^T,  P, dS as above,  dV^T += dO^T P,  dK^T += Q^T dS
-// so that the sums over a group's heads stay in the registers of one wavefront, in fp32 and in a fixed order.
+// so that the sums over a group's heads stay in the registers of one wavefront, in fp32 and in a fixed order.  Where
+// that leaves few and long items (few key heads, long sequences), an item's steps are cut into parts whose sums are joined
+// afterwards, in order.
 // The orientations are chosen so that P and dS go back into the matrix cores as operands without passing through LDS.
 #pragma once
 #include "causal_fwd_kernel.h"
@@ -151,6 +153,12 @@ struct CausalDkvLds {
   } ring[2];
 };
 
+// Where a wavefront's sums for dK stand, in quads of floats; those for dV are 32 D quads behind.
+template <int D>
+__device__ __forceinline__ int64_t part_place(const CausalArgs& a, int rank, int kvh, int part, int wave) {
+  return ((((int64_t)rank * a.kv_heads + kvh) * a.parts + part) * 2 * 4 + wave) * (D / 32 * 4 * 64);
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads, 2) void causal_dkv_kernel(const CausalArgs a) {
   constexpr int NT = D / 16, NC = D / 32;
@@ -159,27 +167,38 @@ __global__ __launch_bounds__(kThreads, 2) void causal_dkv_kernel(const CausalArg
   const RowRead rr(ln, g);
   const ColRead cr(lane);
   const float c2 = a.scale * kLog2e;
+  const int round = a.parts > 1 ? causal_count(a) * a.kv_heads : 0x7fffffff;  // the items' first parts, then their second ones, ..
   for (int item = blockIdx.x;; item += gridDim.x) {
-    const int rank = item / a.kv_heads;
-    TileItem ti = causal_tile(a, rank);
+    const int part = item / round, index = item - part * round;
+    if (part >= a.parts) return;
+    const int rank = index / a.kv_heads, kvh = index - rank * a.kv_heads;
+    const TileItem ti = causal_tile(a, rank);
     if (ti.len == 0) return;
-    const int kvh = item - rank * a.kv_heads, len = ti.len;
+    const int len = ti.len;
     // the tiles' order counts from the sequence's end here
     const int k0 = ((len + kTileRows - 1) / kTileRows - 1) * kTileRows - ti.row0, w0 = k0 + 32 * wave;
-    const int qt0 = k0 / kCausalQueries, nq = (len + kCausalQueries - 1) / kCausalQueries - qt0, n = nq * a.group;
-    int f_head = kvh * a.group, f_qt = 0;  // what is requested next
+    const int qt0 = k0 / kCausalQueries, nq = (len + kCausalQueries - 1) / kCausalQueries - qt0, steps = nq * a.group;
+    const int parts = causal_parts(a, steps);
+    if (part >= parts) continue;
+    const int begin = part * a.chunk, n = part == parts - 1 ? steps - begin : a.chunk;
+    // Blocks from the sequence's end to the diagonal, and all heads of the group block by block: workgroups on different
+    // keys then read the same queries at the same time, from L2 (16384 tokens, 32 / 8 heads of 128: the backward takes 6916 us;
+    // 7119 with the blocks from the diagonal on, head by head; 8270 where parts of items began at different queries).
+    const int h0 = kvh * a.group;
+    int f_head = begin % a.group, f_qt = qt0 + nq - 1 - begin / a.group;  // what is requested next
+    int head = f_head, qt = f_qt;
     auto request = [&](int stage) {
-      const int row = (qt0 + f_qt) * kCausalQueries;
+      const int row = f_qt * kCausalQueries, fh = h0 + f_head;
       const uint32_t at = lds_addr(&lds.ring[stage].q[0]);
-      dma_block<D, kCausalQueries>(a.q + (int64_t)ti.r0 * a.q_stride + f_head * D, a.q_stride, row, len - 1, wave, at);
-      dma_block<D, kCausalQueries>(a.d_o + (int64_t)ti.r0 * a.do_stride + f_head * D, a.do_stride, row, len - 1, wave,
+      dma_block<D, kCausalQueries>(a.q + (int64_t)ti.r0 * a.q_stride + fh * D, a.q_stride, row, len - 1, wave, at);
+      dma_block<D, kCausalQueries>(a.d_o + (int64_t)ti.r0 * a.do_stride + fh * D, a.do_stride, row, len - 1, wave,
                                    lds_addr(&lds.ring[stage].g[0]));
       const int q = row + (lane & 31);
-      const int64_t si = q < len ? (int64_t)f_head * a.total + ti.r0 + q : (int64_t)a.heads * a.total;
+      const int64_t si = q < len ? (int64_t)fh * a.total + ti.r0 + q : (int64_t)a.heads * a.total;
       dma4((lane < 32 ? a.lse2 : a.dsum) + si, __builtin_amdgcn_readfirstlane(lds_addr(&lds.ring[stage].stat[wave][0])));
-      if (++f_qt == nq) {
-        f_qt = 0;
-        f_head++;
+      if (++f_head == a.group) {
+        f_head = 0;
+        f_qt--;
       }
     };
     if (D == 128) {
@@ -212,13 +231,16 @@ __global__ __launch_bounds__(kThreads, 2) void causal_dkv_kernel(const CausalArg
       for (int r = 0; r < 16; r++) dk[cb][r] = dv[cb][r] = 0.f;
     const uint16_t* myk = &lds.k[0] + (wave >> 1) * (64 * D);
 
-    int stage = 0, qt = 0;
+    int stage = 0;
     for (int i = 0; i < n; i++) {
       wait_vmem<0>();
       __syncthreads();
       if (i + 1 < n) request(1 - stage);
-      const int q0 = (qt0 + qt) * kCausalQueries;
-      if (++qt == nq) qt = 0;
+      const int q0 = qt * kCausalQueries;
+      if (++head == a.group) {
+        head = 0;
+        qt--;
+      }
       if (w0 < len && q0 >= w0) {
         const auto& st = lds.ring[stage];
         f32x16 s, dp;
@@ -259,7 +281,16 @@ __global__ __launch_bounds__(kThreads, 2) void causal_dkv_kernel(const CausalArg
       stage = 1 - stage;
     }
     __syncthreads();
-    if (w0 < len) {
+    if (w0 < len && parts > 1) {
+      f32x4* out = reinterpret_cast<f32x4*>(a.part_sums) + part_place<D>(a, rank, kvh, part, wave) + lane;
+#pragma unroll
+      for (int cb = 0; cb < NC; cb++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          out[(4 * cb + j) * 64] = f32x4{dk[cb][4 * j], dk[cb][4 * j + 1], dk[cb][4 * j + 2], dk[cb][4 * j + 3]};
+          out[(4 * cb + j) * 64 + D * 32] = f32x4{dv[cb][4 * j], dv[cb][4 * j + 1], dv[cb][4 * j + 2], dv[cb][4 * j + 3]};
+        }
+    } else if (w0 < len) {
       uint16_t* scratch = &lds.ring[0].q[0] + 2048 * wave;
       static_assert(sizeof(lds.ring) >= 4 * 4096, "scratch of four wavefronts");
       const int64_t tok = ti.r0 + w0;
@@ -271,6 +302,48 @@ __global__ __launch_bounds__(kThreads, 2) void causal_dkv_kernel(const CausalArg
       }
     }
     __syncthreads();
+  }
+}
+
+// dK and dV of the items that were cut: the parts' sums in order.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void causal_dkv_join_kernel(const CausalArgs a) {
+  __shared__ __align__(16) uint16_t scratch[4][2048];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  for (int item = blockIdx.x;; item += gridDim.x) {
+    const int rank = item / a.kv_heads, kvh = item - rank * a.kv_heads;
+    const TileItem ti = causal_tile(a, rank);
+    if (ti.len == 0) return;
+    const int len = ti.len, k0 = ((len + kTileRows - 1) / kTileRows - 1) * kTileRows - ti.row0, w0 = k0 + 32 * wave;
+    const int nq = (len + kCausalQueries - 1) / kCausalQueries - k0 / kCausalQueries;
+    const int parts = causal_parts(a, nq * a.group);
+    if (parts == 1 || w0 >= len) continue;
+    const int64_t tok = ti.r0 + w0, step = part_place<D>(a, rank, kvh, 1, wave) - part_place<D>(a, rank, kvh, 0, wave);
+#pragma unroll
+    for (int which = 0; which < 2; which++) {
+      const f32x4* src = reinterpret_cast<const f32x4*>(a.part_sums) + part_place<D>(a, rank, kvh, 0, wave) + which * D * 32 + lane;
+#pragma unroll
+      for (int h = 0; h < D / 64; h++) {
+        f32x16 x[2];
+#pragma unroll
+        for (int cb = 0; cb < 2; cb++)
+#pragma unroll
+          for (int r = 0; r < 16; r++) x[cb][r] = 0.f;
+#pragma unroll 2
+        for (int p = 0; p < parts; p++) {
+#pragma unroll
+          for (int cb = 0; cb < 2; cb++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+              const f32x4 y = src[p * step + (4 * (2 * h + cb) + j) * 64];
+#pragma unroll
+              for (int e = 0; e < 4; e++) x[cb][4 * j + e] += y[e];
+            }
+        }
+        store_rows32<T>(x, which ? 1.f : a.scale, scratch[wave], which ? a.dv : a.dk,
+                        tok * (which ? a.dv_stride : a.dk_stride) + kvh * D + 64 * h, which ? a.dv_stride : a.dk_stride, len - w0);
+      }
+    }
   }
 }
 

@@ -106,6 +106,8 @@ CASES = [  # lens, heads, kv_heads, D
     ([5, 0, 140] * 23, 2, 1, 64),         # more sequences than a wavefront has lanes: the list
     ([129, 7, 0, 64, 1] * 60, 1, 1, 128),
     ([2500], 2, 1, 64),
+    ([1500], 8, 1, 128),                  # few key heads: the dK/dV pass in parts
+    ([40, 1100, 0, 300], 12, 2, 64),
 ]
 
 
@@ -227,7 +229,8 @@ def test_wrong_bounds_on_the_length():
                 x.fill_(float("nan"))
             b.fwd(longest=longest)
             b.bwd(longest=longest)
-            assert all(torch.equal(x, w) for x, w in zip(b.outputs(), want)), longest
+            assert all(torch.equal(x, w) for x, w in zip(b.outputs()[:3], want[:3])), longest
+            check(b)  # (dK and dV may be summed in other parts)
 
 
 def test_prefix_sums_that_disagree_with_the_sizes():
