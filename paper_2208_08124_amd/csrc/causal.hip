@@ -142,8 +142,18 @@ unsigned grid_of(const fmha_causal_params_t* p, int heads) {
 // (1280 items of keys) 465 / 408; 8 x 4096, 32 / 32 heads of 128, forward (8192) 1160 / 1566.
 constexpr unsigned kByCost = 2048;
 
-int launch_list(const fmha_causal_params_t* p, const fmha::CausalArgs& a, hipStream_t st) {
-  if (p->batch <= fmha::kCausalSelf || (p->flags & FMHA_FLAG_REUSE_SCHEDULE)) return FMHA_OK;
+// Whether all sequences are (said to be) of one tile: the forward's items are then sequences, and nothing is looked up
+// (256 x 43 .. 128 tokens, 16 heads of 64: 43 us with tiles and their list, 35 so).
+bool whole(const fmha_causal_params_t* p) { return p->max_seqlen > 0 && p->max_seqlen <= fmha::kTileRows; }
+
+// Whether the backward takes them as sequences, too: one workgroup then does all of a sequence's queries and heads of a
+// group, so there should be enough of them, and no group.  us, two passes / whole, heads of 64: 256 x 128 tokens, 16 / 16 heads
+// 212 / 165; 64 x 20 .. 60, 16 / 16 26 / 22; 4 x 33 .. 100, 12 / 4 23 / 29; 30 x 43 .. 128, 64 / 1 107 / 700; of 128:
+// 256 x 43 .. 128, 32 / 8 364 / 386.
+bool whole_bwd(const fmha_causal_params_t* p) { return whole(p) && p->heads == p->kv_heads && (int64_t)p->batch * p->heads >= 512; }
+
+int launch_list(const fmha_causal_params_t* p, const fmha::CausalArgs& a, bool needed, hipStream_t st) {
+  if (!needed || p->batch <= fmha::kCausalSelf || (p->flags & FMHA_FLAG_REUSE_SCHEDULE)) return FMHA_OK;
   const Workspace w = carve(p->batch, p->total_tokens, p->heads, p->kv_heads, p->head_dim);
   char* base = static_cast<char*>(p->workspace);
   fmha::causal_list_kernel<<<2, fmha::kCausalListThreads, 0, st>>>(a, reinterpret_cast<int32_t*>(base),
@@ -170,7 +180,8 @@ unsigned plan(const fmha_causal_params_t* p, int heads, fmha::CausalArgs* a) {
 
 template <typename T, int D>
 int launch_fwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st) {
-  const unsigned grid = plan(p, a.heads, &a);
+  a.whole = whole(p);
+  const unsigned grid = a.whole ? (unsigned)(p->batch * a.heads) : plan(p, a.heads, &a);
   fmha::causal_fwd_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal forward launch failed: %s", hipGetErrorString(e));
@@ -179,6 +190,12 @@ int launch_fwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st
 
 template <typename T, int D>
 int launch_bwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st) {
+  if (whole_bwd(p)) {
+    fmha::causal_bwd_whole_kernel<T, D><<<(unsigned)(p->batch * a.kv_heads), fmha::kThreads, 0, st>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal backward launch failed: %s", hipGetErrorString(e));
+    return FMHA_OK;
+  }
   unsigned grid = plan(p, a.heads, &a);
   fmha::causal_dq_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
@@ -223,7 +240,7 @@ int fmha_causal_fwd(const fmha_causal_params_t* p, const void* q, const void* k,
   a.o = out(o);
   a.lse = lse;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if ((rc = launch_list(p, a, st))) return rc;
+  if ((rc = launch_list(p, a, !whole(p), st))) return rc;
   if (p->dtype == FMHA_F16) return p->head_dim == 64 ? launch_fwd<_Float16, 64>(p, a, st) : launch_fwd<_Float16, 128>(p, a, st);
   return p->head_dim == 64 ? launch_fwd<__bf16, 64>(p, a, st) : launch_fwd<__bf16, 128>(p, a, st);
 }
@@ -249,7 +266,7 @@ int fmha_causal_bwd(const fmha_causal_params_t* p, const void* q, const void* k,
   a.dk = out(dk);
   a.dv = out(dv);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if ((rc = launch_list(p, a, st))) return rc;
+  if ((rc = launch_list(p, a, !whole_bwd(p), st))) return rc;
   if (p->dtype == FMHA_F16) return p->head_dim == 64 ? launch_bwd<_Float16, 64>(p, a, st) : launch_bwd<_Float16, 128>(p, a, st);
   return p->head_dim == 64 ? launch_bwd<__bf16, 64>(p, a, st) : launch_bwd<__bf16, 128>(p, a, st);
 }

@@ -6,20 +6,23 @@
 //   by sequence  the sequences as they are packed, the tiles of each by falling j.  The tiles that run at a time then share their
 //                keys in L2: 8 x 4096 tokens, 32 / 32 heads of 128, forward 1160 us against 1566 by cost.
 //   by cost      all tiles by falling j, for launches of few items: long ones first, short ones fill the tail.
+// Where all sequences are said to be of one tile, an item is a whole sequence and nothing has to be looked up (a
+// longer one, if there is one after all, is then one workgroup's work, tile by tile).
 #pragma once
 #include "kernel_args.h"
 #include "mfma_tiles.h"
 
 namespace fmha {
 
-constexpr int kCausalSelf = 64;  // sequences up to which a kernel works the order out by itself, one lane each
+constexpr int kCausalSelf = 256;  // sequences up to which a kernel works the order out by itself, up to four to a lane
 
 struct CausalArgs {
   const int32_t* cu;
   int32_t batch, total;
   int32_t heads, kv_heads, group;
   float scale;
-  int32_t by_cost;       // the order
+  int32_t whole;         // items are whole sequences
+  int32_t by_cost;       // the order of tiles
   const TileItem* list;  // in that order; null: the kernel looks for itself
   const int32_t* count;
   const uint16_t *q, *k, *v, *o_in, *d_o;
@@ -35,6 +38,26 @@ struct CausalArgs {
 // Parts of an item of n steps (at most a.parts, the last takes what is left): the others have `chunk`, so that the parts of all tiles of a sequence begin at the same queries.
 __device__ __forceinline__ int causal_parts(const CausalArgs& a, int n) {
   return a.parts == 1 ? 1 : min(a.parts, (n + a.chunk - 1) / a.chunk);
+}
+
+// Over a lane and the one 32 away, in both: v_permlane32_swap hands each of them the pair, in one order or the other.  (Its
+// two operands are kept apart: given one and the same, the compiler takes its two results for one and the same.)
+__device__ __forceinline__ void pair_of(float x, float& a, float& b) {
+  uint32_t u = __builtin_bit_cast(uint32_t, x), v = u;
+  asm("" : "+v"(v));
+  const auto r = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+  a = __builtin_bit_cast(float, (uint32_t)r[0]);
+  b = __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  float a, b;
+  pair_of(x, a, b);
+  return a + b;
+}
+__device__ __forceinline__ float pair_max(float x) {
+  float a, b;
+  pair_of(x, a, b);
+  return fmaxf(a, b);
 }
 
 // Sum over the lanes up to each.
@@ -55,22 +78,42 @@ __device__ __forceinline__ void causal_sequence(const CausalArgs& a, int i, int&
   len = min(max(a.cu[i + 1], r0), a.total) - r0;
 }
 
-// The tile of rank `rank` (len = 0: there is none), for up to 64 sequences.  By cost: with C(j) = the number of tiles with an
+// A lane's share of the sequences: n neighbouring ones.
+struct CausalLane {
+  int n;  // sequences a lane has
+  int r0[4], len[4], nt[4];
+  __device__ __forceinline__ explicit CausalLane(const CausalArgs& a) {
+    const int lane = lane_id();
+    n = (a.batch + 63) >> 6;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      r0[i] = len[i] = 0;
+      if (i < n && lane * n + i < a.batch) causal_sequence(a, lane * n + i, r0[i], len[i]);
+      nt[i] = (len[i] + kTileRows - 1) / kTileRows;
+    }
+  }
+  // tiles with an index of at least j
+  __device__ __forceinline__ int from(int j) const {
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) c += max(nt[i] - j, 0);
+    return c;
+  }
+};
+
+// The tile of rank `rank` (len = 0: there is none), for up to 256 sequences.  By cost: with C(j) = the number of tiles with an
 // index of at least j, its index is the largest j with C(j) > rank, and it is number rank - C(j + 1) of the sequences
 // that have such a tile.
 __device__ __forceinline__ TileItem causal_find(const CausalArgs& a, int rank) {
-  const int lane = threadIdx.x & 63;
-  int r0 = 0, len = 0;
-  if (lane < a.batch) causal_sequence(a, lane, r0, len);
-  const int nt = (len + kTileRows - 1) / kTileRows;
-  const int upto = wave_scan(nt);
-  const uint64_t past = __ballot(upto > rank);
+  const CausalLane me(a);
+  const int upto = wave_scan(me.from(0));
+  uint64_t past = __ballot(upto > rank);
   if (!past) return TileItem{0, 0, 0, 0};
-  int who = __builtin_ctzll(past), j = __builtin_amdgcn_readlane(upto, who) - 1 - rank;
+  int who, skip, j = -1;
   if (a.by_cost && a.batch > 1) {
     int lo = 0, hi = (a.total + kTileRows - 1) / kTileRows, above = 0;  // C(lo) > rank >= C(hi) = above
     while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1, c = wave_sum(max(nt - mid, 0));
+      const int mid = (lo + hi) >> 1, c = wave_sum(me.from(mid));
       if (c > rank) {
         lo = mid;
       } else {
@@ -78,12 +121,32 @@ __device__ __forceinline__ TileItem causal_find(const CausalArgs& a, int rank) {
         above = c;
       }
     }
-    uint64_t have = __ballot(nt > lo);
-    for (int skip = rank - above; skip > 0; skip--) have &= have - 1;
-    who = __builtin_ctzll(have);
+    int have = 0;  // of the lane's sequences
+#pragma unroll
+    for (int i = 0; i < 4; i++) have += me.nt[i] > lo;
+    const int to = wave_scan(have);
+    past = __ballot(to > rank - above);
+    who = __builtin_ctzll(past);
+    skip = rank - above - (__builtin_amdgcn_readlane(to, who) - __builtin_amdgcn_readlane(have, who));
     j = lo;
+  } else {
+    who = __builtin_ctzll(past);
+    skip = rank - (__builtin_amdgcn_readlane(upto, who) - __builtin_amdgcn_readlane(me.from(0), who));
   }
-  return TileItem{__builtin_amdgcn_readlane(r0, who), __builtin_amdgcn_readlane(len, who), 0, j * kTileRows};
+  // the lane's sequence: the first one whose tiles reach beyond `skip`
+  TileItem ti = {0, 0, 0, 0};
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const int nt = __builtin_amdgcn_readlane(me.nt[i], who), count = j < 0 ? nt : (nt > j);
+    if (!found && skip < count) {
+      found = true;
+      ti = TileItem{__builtin_amdgcn_readlane(me.r0[i], who), __builtin_amdgcn_readlane(me.len[i], who), 0,
+                    (j < 0 ? nt - 1 - skip : j) * kTileRows};
+    }
+    skip -= count;
+  }
+  return ti;
 }
 
 __device__ __forceinline__ TileItem causal_tile(const CausalArgs& a, int rank) {
@@ -96,10 +159,7 @@ __device__ __forceinline__ TileItem causal_tile(const CausalArgs& a, int rank) {
 // Number of tiles.
 __device__ __forceinline__ int causal_count(const CausalArgs& a) {
   if (a.list) return *(ConstInt)(uintptr_t)a.count;
-  const int lane = threadIdx.x & 63;
-  int r0 = 0, len = 0;
-  if (lane < a.batch) causal_sequence(a, lane, r0, len);
-  return wave_sum((len + kTileRows - 1) / kTileRows);
+  return wave_sum(CausalLane(a).from(0));
 }
 
 // The same for more sequences, as lists: count <- number of tiles, by_sequence and by_cost <- the tiles.  A workgroup for each list.

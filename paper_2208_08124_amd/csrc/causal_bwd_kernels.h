@@ -12,6 +12,8 @@
 
 namespace fmha {
 
+constexpr int kCausalKeys = 64;  // keys of a block of the dQ pass
+
 template <typename T>
 __device__ __forceinline__ u32x4 pack_half(const float (&x)[16], int t2) {
   return u32x4{Op<T>::pack2(x[8 * t2], x[8 * t2 + 1]), Op<T>::pack2(x[8 * t2 + 2], x[8 * t2 + 3]),
@@ -20,122 +22,156 @@ __device__ __forceinline__ u32x4 pack_half(const float (&x)[16], int t2) {
 
 // ------------------------------------------------------------------ dQ
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void causal_dq_kernel(const CausalArgs a) {
-  constexpr int NST = kCausalStages<D>, NT = D / 16, NC = D / 32;
+__device__ __forceinline__ void causal_dq_tile(const CausalArgs& a, CausalFwdLds<D, kCausalKeys>& lds, const TileItem& ti, int head, int wave) {
+  constexpr int NT = D / 16, NC = D / 32;
   constexpr uint32_t kHalfBytes = kCausalKeys * D * 2;
-  constexpr int kPieces = 2 * (D / 64) * 2;
-  __shared__ __align__(1024) CausalFwdLds<T, D> lds;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+  const int lane = lane_id(), g = lane >> 5, ln = lane & 31;
   const RowRead rr(ln, g);
   const ColRead cr(lane);
   const uint32_t ring_addr = lds_addr(&lds.ring[0][0][0]);
   const float c2 = a.scale * kLog2e;
-  // "row past the end" in the dK/dV pass: its probabilities vanish
-  if (blockIdx.x == 0 && tid == 0) {
+  const int kvh = head / a.group;
+  const int len = ti.len, row0 = ti.row0, w0 = row0 + 32 * wave;
+  const uint16_t* kbase = a.k + (int64_t)ti.r0 * a.k_stride + kvh * D;
+  const uint16_t* vbase = a.v + (int64_t)ti.r0 * a.v_stride + kvh * D;
+  const int keys = min(len, row0 + kTileRows), n = (keys + kCausalKeys - 1) / kCausalKeys;
+  const int mine = w0 < len ? w0 / kCausalKeys + 1 : 0;
+  const bool first = row0 == 0;  // (no more than two blocks of keys: both places of the ring)
+  auto request = [&](int kt, int stage) {
+    const uint32_t at = ring_addr + stage * (2 * kHalfBytes);
+    dma_block<D, kCausalKeys>(kbase, a.k_stride, kt * kCausalKeys, len - 1, wave, at);
+    dma_block<D, kCausalKeys>(vbase, a.v_stride, kt * kCausalKeys, len - 1, wave, at + kHalfBytes);
+  };
+  request(0, 0);
+  if (first && n > 1) request(1, 1);
+
+  // Q^T, dO^T as operands (column = query ln), D of the query, its LSE
+  u32x4 qb[NT], gb[NT];
+  float dsum = 0.f, lse2;
+  {
+    const int64_t tok = ti.r0 + min(w0 + ln, len - 1);
+    const uint16_t* qp = a.q + tok * a.q_stride + head * D + 8 * g;
+    const uint16_t* gp = a.d_o + tok * a.do_stride + head * D + 8 * g;
+    const uint16_t* op = a.o_in + tok * a.o_stride + head * D + 8 * g;
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      qb[t] = *reinterpret_cast<const u32x4*>(qp + 16 * t);
+      gb[t] = *reinterpret_cast<const u32x4*>(gp + 16 * t);
+      const u32x4 ov = *reinterpret_cast<const u32x4*>(op + 16 * t);
+#pragma unroll
+      for (int e = 0; e < 4; e++) dsum = Op<T>::dot2(gb[t][e], ov[e], dsum);
+    }
+    dsum = pair_sum(dsum);
+    lse2 = a.lse[(int64_t)head * a.total + tok] * kLog2e;
+#pragma unroll
+    for (int t = 0; t < NT; t++) asm volatile("" ::"v"(qb[t]), "v"(gb[t]));
+    asm volatile("" ::"v"(dsum), "v"(lse2));
+  }
+  f32x16 dq[NC];
+#pragma unroll
+  for (int cb = 0; cb < NC; cb++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) dq[cb][r] = 0.f;
+
+  auto scores = [&](int kt, int kb, f32x16& s, f32x16& dp) {
+    const uint16_t *sK = &lds.ring[kt & 1][0][0], *sV = &lds.ring[kt & 1][1][0];
+#pragma unroll
+    for (int r = 0; r < 16; r++) s[r] = dp[r] = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      s = Op<T>::mfma(read_rows<D, kCausalKeys>(rr, sK, kb, t), qb[t], s);
+      dp = Op<T>::mfma(read_rows<D, kCausalKeys>(rr, sV, kb, t), gb[t], dp);
+    }
+  };
+  // rowsum(dO o O) carries the rounding of the stored O, which tells where few keys share a row: a row of n keys has an O, and
+  // with it that error, of about 1 / sqrt(n) of a V.  The first tile's rows take D = rowsum(P o dP), which is the same without it,
+  // from a sweep of their own over their two blocks.
+  if (first) {
+    wait_vmem<0>();
+    __syncthreads();
+    float more = 0.f;
+    for (int kt = 0; kt < mine; kt++) {
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++) {
+        const int key0 = kt * kCausalKeys + 32 * kb;
+        if (key0 > w0) break;
+        f32x16 s, dp;
+        scores(kt, kb, s, dp);
+        const int le = lane_id(), room = key0 == w0 ? (le & 31) - 4 * (le >> 5) : 32;
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+          if (8 * (r >> 2) + (r & 3) <= room) more += fast_exp2(__builtin_fmaf(s[r], c2, -lse2)) * (dp[r] - dsum);
+      }
+    }
+    dsum += pair_sum(more);
+  }
+  for (int kt = 0; kt < n; kt++) {
+    if (!first) {
+      wait_vmem<0>();
+      __syncthreads();
+      if (kt + 1 < n) request(kt + 1, (kt + 1) & 1);
+    }
+    if (kt < mine) {
+      const uint16_t* sK = &lds.ring[kt & 1][0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++) {
+        const int key0 = kt * kCausalKeys + 32 * kb;
+        if (key0 > w0) break;  // (blocks of 32 line up with the wavefronts' queries)
+        f32x16 s, dp;
+        scores(kt, kb, s, dp);
+        float ds[16];
+#pragma unroll
+        for (int r = 0; r < 16; r++) ds[r] = fast_exp2(__builtin_fmaf(s[r], c2, -lse2)) * (dp[r] - dsum);
+        if (key0 == w0) {  // the diagonal
+          const int le = lane_id(), room = (le & 31) - 4 * (le >> 5);
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (8 * (r >> 2) + (r & 3) > room) ds[r] = 0.f;
+        }
+        const u32x4 dsb[2] = {pack_half<T>(ds, 0), pack_half<T>(ds, 1)};
+#pragma unroll
+        for (int t2 = 0; t2 < 2; t2++)
+#pragma unroll
+          for (int cb = 0; cb < NC; cb++) dq[cb] = Op<T>::mfma(read_cols<D, kCausalKeys>(cr, sK, 2 * kb + t2, cb), dsb[t2], dq[cb]);
+      }
+    }
+  }
+  __syncthreads();
+  if (mine) {
+    const int le = lane_id();
+    if (le < 32 && w0 + le < len) {
+      const int64_t si = (int64_t)head * a.total + ti.r0 + w0 + le;
+      a.dsum[si] = -dsum;
+      a.lse2[si] = lse2;
+    }
+    uint16_t* scratch = &lds.ring[0][0][0] + 2048 * wave;
+#pragma unroll
+    for (int h = 0; h < D / 64; h++) {
+      const f32x16 x[2] = {dq[2 * h], dq[2 * h + 1]};
+      store_rows32<T>(x, a.scale, scratch, a.dq, (int64_t)(ti.r0 + w0) * a.dq_stride + head * D + 64 * h, a.dq_stride, len - w0);
+    }
+  }
+  __syncthreads();
+}
+
+// "row past the end" in the dK/dV pass: its probabilities vanish
+__device__ __forceinline__ void causal_pad(const CausalArgs& a) {
+  if (threadIdx.x == 0) {
     a.lse2[(int64_t)a.heads * a.total] = INFINITY;
     a.dsum[(int64_t)a.heads * a.total] = 0.f;
   }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void causal_dq_kernel(const CausalArgs a) {
+  __shared__ __align__(1024) CausalFwdLds<D, kCausalKeys> lds;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (blockIdx.x == 0) causal_pad(a);
   for (int item = blockIdx.x;; item += gridDim.x) {
     const int rank = item / a.heads;
     const TileItem ti = causal_tile(a, rank);
     if (ti.len == 0) return;
-    const int head = causal_head(item - rank * a.heads, a.heads, a.kv_heads, a.group), kvh = head / a.group;
-    const int len = ti.len, row0 = ti.row0, w0 = row0 + 32 * wave;
-    const uint16_t* kbase = a.k + (int64_t)ti.r0 * a.k_stride + kvh * D;
-    const uint16_t* vbase = a.v + (int64_t)ti.r0 * a.v_stride + kvh * D;
-    const int keys = min(len, row0 + kTileRows), n = (keys + kCausalKeys - 1) / kCausalKeys;
-    const int mine = w0 < len ? w0 / kCausalKeys + 1 : 0;
-    auto request = [&](int kt, int stage) {
-      const uint32_t at = ring_addr + stage * (2 * kHalfBytes);
-      dma_block<D, kCausalKeys>(kbase, a.k_stride, kt * kCausalKeys, len - 1, wave, at);
-      dma_block<D, kCausalKeys>(vbase, a.v_stride, kt * kCausalKeys, len - 1, wave, at + kHalfBytes);
-    };
-    request(0, 0);
-    if (NST == 3 && n > 1) request(1, 1);
-
-    // Q^T, dO^T as operands (column = query ln), D of the query, its LSE
-    u32x4 qb[NT], gb[NT];
-    float dsum = 0.f, lse2;
-    {
-      const int64_t tok = ti.r0 + min(w0 + ln, len - 1);
-      const uint16_t* qp = a.q + tok * a.q_stride + head * D + 8 * g;
-      const uint16_t* gp = a.d_o + tok * a.do_stride + head * D + 8 * g;
-      const uint16_t* op = a.o_in + tok * a.o_stride + head * D + 8 * g;
-#pragma unroll
-      for (int t = 0; t < NT; t++) {
-        qb[t] = *reinterpret_cast<const u32x4*>(qp + 16 * t);
-        gb[t] = *reinterpret_cast<const u32x4*>(gp + 16 * t);
-        const u32x4 ov = *reinterpret_cast<const u32x4*>(op + 16 * t);
-#pragma unroll
-        for (int e = 0; e < 4; e++) dsum = Op<T>::dot2(gb[t][e], ov[e], dsum);
-      }
-      dsum += other_half(dsum);
-      lse2 = a.lse[(int64_t)head * a.total + tok] * kLog2e;
-#pragma unroll
-      for (int t = 0; t < NT; t++) asm volatile("" ::"v"(qb[t]), "v"(gb[t]));
-      asm volatile("" ::"v"(dsum), "v"(lse2));
-    }
-    f32x16 dq[NC];
-#pragma unroll
-    for (int cb = 0; cb < NC; cb++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) dq[cb][r] = 0.f;
-
-    int stage = 0;
-    for (int kt = 0; kt < n; kt++) {
-      if (NST == 3 && kt + 1 < n)
-        wait_vmem<kPieces>();
-      else
-        wait_vmem<0>();
-      __syncthreads();
-      const int ahead = NST == 3 ? (stage == 0 ? 2 : stage - 1) : 1 - stage;
-      if (kt + NST - 1 < n) request(kt + NST - 1, ahead);
-      if (kt < mine) {
-        const uint16_t *sK = &lds.ring[stage][0][0], *sV = &lds.ring[stage][1][0];
-#pragma unroll
-        for (int kb = 0; kb < 2; kb++) {
-          const int key0 = kt * kCausalKeys + 32 * kb;
-          if (key0 > w0) break;  // (blocks of 32 line up with the wavefronts' queries)
-          f32x16 s, dp;
-#pragma unroll
-          for (int r = 0; r < 16; r++) s[r] = dp[r] = 0.f;
-#pragma unroll
-          for (int t = 0; t < NT; t++) {
-            s = Op<T>::mfma(read_rows<D, kCausalKeys>(rr, sK, kb, t), qb[t], s);
-            dp = Op<T>::mfma(read_rows<D, kCausalKeys>(rr, sV, kb, t), gb[t], dp);
-          }
-          float ds[16];
-#pragma unroll
-          for (int r = 0; r < 16; r++) ds[r] = fast_exp2(__builtin_fmaf(s[r], c2, -lse2)) * (dp[r] - dsum);
-          if (key0 == w0) {  // the diagonal
-#pragma unroll
-            for (int r = 0; r < 16; r++)
-              if (8 * (r >> 2) + 4 * g + (r & 3) > ln) ds[r] = 0.f;
-          }
-          const u32x4 dsb[2] = {pack_half<T>(ds, 0), pack_half<T>(ds, 1)};
-#pragma unroll
-          for (int t2 = 0; t2 < 2; t2++)
-#pragma unroll
-            for (int cb = 0; cb < NC; cb++) dq[cb] = Op<T>::mfma(read_cols<D, kCausalKeys>(cr, sK, 2 * kb + t2, cb), dsb[t2], dq[cb]);
-        }
-      }
-      stage = NST == 3 ? (stage == 2 ? 0 : stage + 1) : 1 - stage;
-    }
-    __syncthreads();
-    if (mine) {
-      if (lane < 32 && w0 + ln < len) {
-        const int64_t si = (int64_t)head * a.total + ti.r0 + w0 + ln;
-        a.dsum[si] = -dsum;
-        a.lse2[si] = lse2;
-      }
-      uint16_t* scratch = &lds.ring[0][0][0] + 2048 * wave;
-#pragma unroll
-      for (int h = 0; h < D / 64; h++) {
-        const f32x16 x[2] = {dq[2 * h], dq[2 * h + 1]};
-        store_rows32<T>(x, a.scale, scratch, a.dq, (int64_t)(ti.r0 + w0) * a.dq_stride + head * D + 64 * h, a.dq_stride, len - w0);
-      }
-    }
-    __syncthreads();
+    causal_dq_tile<T, D>(a, lds, ti, causal_head(item - rank * a.heads, a.heads, a.kv_heads, a.group), wave);
   }
 }
 
@@ -159,14 +195,146 @@ __device__ __forceinline__ int64_t part_place(const CausalArgs& a, int rank, int
   return ((((int64_t)rank * a.kv_heads + kvh) * a.parts + part) * 2 * 4 + wave) * (D / 32 * 4 * 64);
 }
 
+// Keys k0 .. k0 + 127 of a sequence; part `part` of `parts` of the steps (of a tile of rank `rank`, which parts alone ask for).
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void causal_dkv_kernel(const CausalArgs a) {
+__device__ __forceinline__ void causal_dkv_tile(const CausalArgs& a, CausalDkvLds<D>& lds, const TileItem& ti, int k0, int kvh, int rank,
+                                                int part, int parts, int wave) {
   constexpr int NT = D / 16, NC = D / 32;
-  __shared__ __align__(1024) CausalDkvLds<D> lds;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+  const int lane = lane_id(), g = lane >> 5, ln = lane & 31;
   const RowRead rr(ln, g);
   const ColRead cr(lane);
   const float c2 = a.scale * kLog2e;
+  const int len = ti.len, w0 = k0 + 32 * wave;
+  const int qt0 = k0 / kCausalQueries, nq = (len + kCausalQueries - 1) / kCausalQueries - qt0, steps = nq * a.group;
+  const int begin = part * a.chunk, n = part == parts - 1 ? steps - begin : a.chunk;  // its steps
+  // Blocks from the sequence's end to the diagonal, and all heads of the group block by block: workgroups on different
+  // keys then read the same queries at the same time, from L2 (16384 tokens, 32 / 8 heads of 128: the backward takes 6916 us;
+  // 7119 with the blocks from the diagonal on, head by head; 8270 where parts of items began at different queries).
+  const int h0 = kvh * a.group;
+  int f_head = begin % a.group, f_qt = qt0 + nq - 1 - begin / a.group;  // what is requested next
+  int head = f_head, qt = f_qt;
+  auto request = [&](int stage) {
+    const int row = f_qt * kCausalQueries, fh = h0 + f_head;
+    const uint32_t at = lds_addr(&lds.ring[stage].q[0]);
+    dma_block<D, kCausalQueries>(a.q + (int64_t)ti.r0 * a.q_stride + fh * D, a.q_stride, row, len - 1, wave, at);
+    dma_block<D, kCausalQueries>(a.d_o + (int64_t)ti.r0 * a.do_stride + fh * D, a.do_stride, row, len - 1, wave,
+                                 lds_addr(&lds.ring[stage].g[0]));
+    const int le = lane_id(), q = row + (le & 31);
+    const int64_t si = q < len ? (int64_t)fh * a.total + ti.r0 + q : (int64_t)a.heads * a.total;
+    dma4((le < 32 ? a.lse2 : a.dsum) + si, __builtin_amdgcn_readfirstlane(lds_addr(&lds.ring[stage].stat[wave][0])));
+    if (++f_head == a.group) {
+      f_head = 0;
+      f_qt--;
+    }
+  };
+  if (D == 128) {
+    const uint16_t* kbase = a.k + (int64_t)ti.r0 * a.k_stride + kvh * D;
+    // two blocks of 64 rows; rows behind the end repeat the last one
+    dma_block<D, 64>(kbase, a.k_stride, k0, len - 1, wave, lds_addr(&lds.k[0]));
+    if (k0 + 64 < len) dma_block<D, 64>(kbase, a.k_stride, k0 + 64, len - 1, wave, lds_addr(&lds.k[0]) + 64 * D * 2);
+  }
+  request(0);
+  u32x4 kb4[D == 64 ? NT : 1], vb[NT];
+  {
+    const int64_t tok = ti.r0 + min(w0 + ln, len - 1);
+    const uint16_t* kp = a.k + tok * a.k_stride + kvh * D + 8 * g;
+    const uint16_t* vp = a.v + tok * a.v_stride + kvh * D + 8 * g;
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      vb[t] = *reinterpret_cast<const u32x4*>(vp + 16 * t);
+      if (D == 64) kb4[t] = *reinterpret_cast<const u32x4*>(kp + 16 * t);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; t++) {
+      asm volatile("" ::"v"(vb[t]));
+      if (D == 64) asm volatile("" ::"v"(kb4[t]));
+    }
+  }
+  f32x16 dk[NC], dv[NC];
+#pragma unroll
+  for (int cb = 0; cb < NC; cb++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) dk[cb][r] = dv[cb][r] = 0.f;
+  const uint16_t* myk = &lds.k[0] + (wave >> 1) * (64 * D);
+
+  int stage = 0;
+  for (int i = 0; i < n; i++) {
+    wait_vmem<0>();
+    __syncthreads();
+    if (i + 1 < n) request(1 - stage);
+    const int q0 = qt * kCausalQueries;
+    if (++head == a.group) {
+      head = 0;
+      qt--;
+    }
+    if (w0 < len && q0 >= w0) {
+      const auto& st = lds.ring[stage];
+      f32x16 s, dp;
+#pragma unroll
+      for (int r = 0; r < 16; r++) s[r] = dp[r] = 0.f;
+#pragma unroll
+      for (int t = 0; t < NT; t++) {
+        const u32x4 kk = D == 64 ? kb4[D == 64 ? t : 0] : read_rows<D, 64>(rr, myk, wave & 1, t);
+        s = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.q, 0, t), kk, s);
+        dp = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.g, 0, t), vb[t], dp);
+      }
+      float p[16], ds[16];
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(&st.stat[wave][8 * j + 4 * g]);
+        const f32x4 d4 = *reinterpret_cast<const f32x4*>(&st.stat[wave][32 + 8 * j + 4 * g]);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const int r = 4 * j + e;
+          p[r] = fast_exp2(__builtin_fmaf(s[r], c2, -l4[e]));
+          ds[r] = p[r] * (dp[r] + d4[e]);
+        }
+      }
+      if (q0 == w0) {  // the diagonal: queries ahead of the lane's key
+        const int le = lane_id(), room = (le & 31) - 4 * (le >> 5);
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+          if (8 * (r >> 2) + (r & 3) < room) p[r] = ds[r] = 0.f;
+      }
+      const u32x4 pb[2] = {pack_half<T>(p, 0), pack_half<T>(p, 1)}, dsb[2] = {pack_half<T>(ds, 0), pack_half<T>(ds, 1)};
+#pragma unroll
+      for (int t2 = 0; t2 < 2; t2++)
+#pragma unroll
+        for (int cb = 0; cb < NC; cb++) {
+          dv[cb] = Op<T>::mfma(read_cols<D, kCausalQueries>(cr, st.g, t2, cb), pb[t2], dv[cb]);
+          dk[cb] = Op<T>::mfma(read_cols<D, kCausalQueries>(cr, st.q, t2, cb), dsb[t2], dk[cb]);
+        }
+    }
+    stage = 1 - stage;
+  }
+  __syncthreads();
+  if (w0 < len && parts > 1) {
+    f32x4* out = reinterpret_cast<f32x4*>(a.part_sums) + part_place<D>(a, rank, kvh, part, wave) + lane_id();
+#pragma unroll
+    for (int cb = 0; cb < NC; cb++)
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        out[(4 * cb + j) * 64] = f32x4{dk[cb][4 * j], dk[cb][4 * j + 1], dk[cb][4 * j + 2], dk[cb][4 * j + 3]};
+        out[(4 * cb + j) * 64 + D * 32] = f32x4{dv[cb][4 * j], dv[cb][4 * j + 1], dv[cb][4 * j + 2], dv[cb][4 * j + 3]};
+      }
+  } else if (w0 < len) {
+    uint16_t* scratch = &lds.ring[0].q[0] + 2048 * wave;
+    static_assert(sizeof(lds.ring) >= 4 * 4096, "scratch of four wavefronts");
+    const int64_t tok = ti.r0 + w0;
+#pragma unroll
+    for (int h = 0; h < D / 64; h++) {
+      const f32x16 x[2] = {dk[2 * h], dk[2 * h + 1]}, y[2] = {dv[2 * h], dv[2 * h + 1]};
+      store_rows32<T>(x, a.scale, scratch, a.dk, tok * a.dk_stride + kvh * D + 64 * h, a.dk_stride, len - w0);
+      store_rows32<T>(y, 1.f, scratch, a.dv, tok * a.dv_stride + kvh * D + 64 * h, a.dv_stride, len - w0);
+    }
+  }
+  __syncthreads();
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void causal_dkv_kernel(const CausalArgs a) {
+  __shared__ __align__(1024) CausalDkvLds<D> lds;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int round = a.parts > 1 ? causal_count(a) * a.kv_heads : 0x7fffffff;  // the items' first parts, then their second ones, ..
   for (int item = blockIdx.x;; item += gridDim.x) {
     const int part = item / round, index = item - part * round;
@@ -174,134 +342,35 @@ __global__ __launch_bounds__(kThreads, 2) void causal_dkv_kernel(const CausalArg
     const int rank = index / a.kv_heads, kvh = index - rank * a.kv_heads;
     const TileItem ti = causal_tile(a, rank);
     if (ti.len == 0) return;
-    const int len = ti.len;
     // the tiles' order counts from the sequence's end here
-    const int k0 = ((len + kTileRows - 1) / kTileRows - 1) * kTileRows - ti.row0, w0 = k0 + 32 * wave;
-    const int qt0 = k0 / kCausalQueries, nq = (len + kCausalQueries - 1) / kCausalQueries - qt0, steps = nq * a.group;
-    const int parts = causal_parts(a, steps);
-    if (part >= parts) continue;
-    const int begin = part * a.chunk, n = part == parts - 1 ? steps - begin : a.chunk;
-    // Blocks from the sequence's end to the diagonal, and all heads of the group block by block: workgroups on different
-    // keys then read the same queries at the same time, from L2 (16384 tokens, 32 / 8 heads of 128: the backward takes 6916 us;
-    // 7119 with the blocks from the diagonal on, head by head; 8270 where parts of items began at different queries).
-    const int h0 = kvh * a.group;
-    int f_head = begin % a.group, f_qt = qt0 + nq - 1 - begin / a.group;  // what is requested next
-    int head = f_head, qt = f_qt;
-    auto request = [&](int stage) {
-      const int row = f_qt * kCausalQueries, fh = h0 + f_head;
-      const uint32_t at = lds_addr(&lds.ring[stage].q[0]);
-      dma_block<D, kCausalQueries>(a.q + (int64_t)ti.r0 * a.q_stride + fh * D, a.q_stride, row, len - 1, wave, at);
-      dma_block<D, kCausalQueries>(a.d_o + (int64_t)ti.r0 * a.do_stride + fh * D, a.do_stride, row, len - 1, wave,
-                                   lds_addr(&lds.ring[stage].g[0]));
-      const int q = row + (lane & 31);
-      const int64_t si = q < len ? (int64_t)fh * a.total + ti.r0 + q : (int64_t)a.heads * a.total;
-      dma4((lane < 32 ? a.lse2 : a.dsum) + si, __builtin_amdgcn_readfirstlane(lds_addr(&lds.ring[stage].stat[wave][0])));
-      if (++f_head == a.group) {
-        f_head = 0;
-        f_qt--;
-      }
-    };
-    if (D == 128) {
-      const uint16_t* kbase = a.k + (int64_t)ti.r0 * a.k_stride + kvh * D;
-      // two blocks of 64 rows; rows behind the end repeat the last one
-      dma_block<D, 64>(kbase, a.k_stride, k0, len - 1, wave, lds_addr(&lds.k[0]));
-      if (k0 + 64 < len) dma_block<D, 64>(kbase, a.k_stride, k0 + 64, len - 1, wave, lds_addr(&lds.k[0]) + 64 * D * 2);
-    }
-    request(0);
-    u32x4 kb4[D == 64 ? NT : 1], vb[NT];
-    {
-      const int64_t tok = ti.r0 + min(w0 + ln, len - 1);
-      const uint16_t* kp = a.k + tok * a.k_stride + kvh * D + 8 * g;
-      const uint16_t* vp = a.v + tok * a.v_stride + kvh * D + 8 * g;
-#pragma unroll
-      for (int t = 0; t < NT; t++) {
-        vb[t] = *reinterpret_cast<const u32x4*>(vp + 16 * t);
-        if (D == 64) kb4[t] = *reinterpret_cast<const u32x4*>(kp + 16 * t);
-      }
-#pragma unroll
-      for (int t = 0; t < NT; t++) {
-        asm volatile("" ::"v"(vb[t]));
-        if (D == 64) asm volatile("" ::"v"(kb4[t]));
-      }
-    }
-    f32x16 dk[NC], dv[NC];
-#pragma unroll
-    for (int cb = 0; cb < NC; cb++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) dk[cb][r] = dv[cb][r] = 0.f;
-    const uint16_t* myk = &lds.k[0] + (wave >> 1) * (64 * D);
+    const int k0 = ((ti.len + kTileRows - 1) / kTileRows - 1) * kTileRows - ti.row0;
+    const int parts = causal_parts(a, ((ti.len + kCausalQueries - 1) / kCausalQueries - k0 / kCausalQueries) * a.group);
+    if (part < parts) causal_dkv_tile<T, D>(a, lds, ti, k0, kvh, rank, part, parts, wave);
+  }
+}
 
-    int stage = 0;
-    for (int i = 0; i < n; i++) {
-      wait_vmem<0>();
-      __syncthreads();
-      if (i + 1 < n) request(1 - stage);
-      const int q0 = qt * kCausalQueries;
-      if (++head == a.group) {
-        head = 0;
-        qt--;
-      }
-      if (w0 < len && q0 >= w0) {
-        const auto& st = lds.ring[stage];
-        f32x16 s, dp;
-#pragma unroll
-        for (int r = 0; r < 16; r++) s[r] = dp[r] = 0.f;
-#pragma unroll
-        for (int t = 0; t < NT; t++) {
-          const u32x4 kk = D == 64 ? kb4[D == 64 ? t : 0] : read_rows<D, 64>(rr, myk, wave & 1, t);
-          s = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.q, 0, t), kk, s);
-          dp = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.g, 0, t), vb[t], dp);
-        }
-        float p[16], ds[16];
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          const f32x4 l4 = *reinterpret_cast<const f32x4*>(&st.stat[wave][8 * j + 4 * g]);
-          const f32x4 d4 = *reinterpret_cast<const f32x4*>(&st.stat[wave][32 + 8 * j + 4 * g]);
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            const int r = 4 * j + e;
-            p[r] = fast_exp2(__builtin_fmaf(s[r], c2, -l4[e]));
-            ds[r] = p[r] * (dp[r] + d4[e]);
-          }
-        }
-        if (q0 == w0) {  // the diagonal: queries ahead of the lane's key
-#pragma unroll
-          for (int r = 0; r < 16; r++)
-            if (8 * (r >> 2) + 4 * g + (r & 3) < ln) p[r] = ds[r] = 0.f;
-        }
-        const u32x4 pb[2] = {pack_half<T>(p, 0), pack_half<T>(p, 1)}, dsb[2] = {pack_half<T>(ds, 0), pack_half<T>(ds, 1)};
-#pragma unroll
-        for (int t2 = 0; t2 < 2; t2++)
-#pragma unroll
-          for (int cb = 0; cb < NC; cb++) {
-            dv[cb] = Op<T>::mfma(read_cols<D, kCausalQueries>(cr, st.g, t2, cb), pb[t2], dv[cb]);
-            dk[cb] = Op<T>::mfma(read_cols<D, kCausalQueries>(cr, st.q, t2, cb), dsb[t2], dk[cb]);
-          }
-      }
-      stage = 1 - stage;
-    }
+// Both for whole sequences: an item is a sequence and a key head, first all of its dQ, then dK and dV.  What the second half reads
+// again is then still in L2, so that short sequences are read from memory once: 256 x 128 tokens, 16 heads of 64, REVUS.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void causal_bwd_whole_kernel(const CausalArgs a) {
+  __shared__ __align__(1024) union Lds {
+    CausalFwdLds<D, kCausalKeys> dq;
+    CausalDkvLds<D> dkv;
+    __device__ Lds() {}
+  } lds;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  causal_pad(a);  // (each for itself: all write the same)
+  for (int item = blockIdx.x;; item += gridDim.x) {
+    const int b = item / a.kv_heads, kvh = item - b * a.kv_heads;
+    if (b >= a.batch) return;
+    TileItem ti = {0, 0, 0, 0};
+    causal_sequence(a, b, ti.r0, ti.len);
+    for (int h = 0; h < a.group; h++)
+      for (ti.row0 = 0; ti.row0 < ti.len; ti.row0 += kTileRows) causal_dq_tile<T, D>(a, lds.dq, ti, kvh * a.group + h, wave);
+    // What the first half left in memory (the statistics) is read by this workgroup alone: it has to have arrived.
+    wait_vmem<0>();
     __syncthreads();
-    if (w0 < len && parts > 1) {
-      f32x4* out = reinterpret_cast<f32x4*>(a.part_sums) + part_place<D>(a, rank, kvh, part, wave) + lane;
-#pragma unroll
-      for (int cb = 0; cb < NC; cb++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          out[(4 * cb + j) * 64] = f32x4{dk[cb][4 * j], dk[cb][4 * j + 1], dk[cb][4 * j + 2], dk[cb][4 * j + 3]};
-          out[(4 * cb + j) * 64 + D * 32] = f32x4{dv[cb][4 * j], dv[cb][4 * j + 1], dv[cb][4 * j + 2], dv[cb][4 * j + 3]};
-        }
-    } else if (w0 < len) {
-      uint16_t* scratch = &lds.ring[0].q[0] + 2048 * wave;
-      static_assert(sizeof(lds.ring) >= 4 * 4096, "scratch of four wavefronts");
-      const int64_t tok = ti.r0 + w0;
-#pragma unroll
-      for (int h = 0; h < D / 64; h++) {
-        const f32x16 x[2] = {dk[2 * h], dk[2 * h + 1]}, y[2] = {dv[2 * h], dv[2 * h + 1]};
-        store_rows32<T>(x, a.scale, scratch, a.dk, tok * a.dk_stride + kvh * D + 64 * h, a.dk_stride, len - w0);
-        store_rows32<T>(y, 1.f, scratch, a.dv, tok * a.dv_stride + kvh * D + 64 * h, a.dv_stride, len - w0);
-      }
-    }
-    __syncthreads();
+    for (int k0 = 0; k0 < ti.len; k0 += kTileRows) causal_dkv_tile<T, D>(a, lds.dkv, ti, k0, kvh, 0, 0, 1, wave);
   }
 }
 

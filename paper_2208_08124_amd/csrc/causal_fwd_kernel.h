@@ -1,7 +1,7 @@
 // Causal forward on packed sequences with grouped heads: O = softmax(scale Q K^T + causal mask) V, one pass over the keys.
 //
 // A workgroup of four wavefronts takes 128 queries of one head, 32 to a wavefront, and goes over the keys up to its last
-// query in blocks of 64, which travel from memory straight into a ring in LDS.  S^T = K Q^T has a lane hold one
+// query in blocks of 32 or 64, which travel from memory straight into a ring in LDS.  S^T = K Q^T has a lane hold one
 // query's scores, so the softmax's maximum and sum are the lane's own (and its partner's 32 lanes on), and the packed
 // probabilities are, in place, the operand of O^T += V^T P^T.  Only blocks that touch the diagonal are masked.
 // The maximum is a running one that is raised, and what has been summed up rescaled, only when a block exceeds it by
@@ -12,14 +12,14 @@
 
 namespace fmha {
 
-constexpr int kCausalKeys = 64;  // keys of a block
-
+// Keys of a block: at 128 channels blocks of 32 leave room for three workgroups on a compute unit, whose starts and ends hide
+// behind one another (64 x 512 tokens, 16 / 4 heads 143 -> 134 us, 16 x 2048, 32 / 8 641 -> 613, 1 x 16384 1960 -> 1970).
 template <int D>
-constexpr int kCausalStages = D == 64 ? 3 : 2;
+constexpr int kFwdKeys = D == 64 ? 64 : 32;
 
-template <typename T, int D>
+template <int D, int KEYS>
 struct CausalFwdLds {
-  uint16_t ring[kCausalStages<D>][2][kCausalKeys * D];  // [stage][K|V]
+  uint16_t ring[2][2][KEYS * D];  // [stage][K|V]
 };
 
 // Key operand: rows 32 kb + ln, channels 16 t + 8 g .. +7
@@ -34,132 +34,143 @@ __device__ __forceinline__ u32x4 read_cols(const ColRead& cr, const uint16_t* ti
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void causal_fwd_kernel(const CausalArgs a) {
-  constexpr int NST = kCausalStages<D>, NT = D / 16, NC = D / 32;
-  constexpr uint32_t kHalfBytes = kCausalKeys * D * 2;  // K or V of a stage
-  constexpr int kPieces = 2 * (D / 64) * 2;             // requests a lane makes per block
-  __shared__ __align__(1024) CausalFwdLds<T, D> lds;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+__device__ __forceinline__ void causal_fwd_tile(const CausalArgs& a, CausalFwdLds<D, kFwdKeys<D>>& lds, const TileItem& ti, int head, int wave) {
+  constexpr int NT = D / 16, NC = D / 32, BK = kFwdKeys<D>, KB = BK / 32;
+  constexpr uint32_t kHalfBytes = BK * D * 2;  // K or V of a stage
+  const int lane = D == 128 ? lane_id() : threadIdx.x & 63, g = lane >> 5, ln = lane & 31;
   const RowRead rr(ln, g);
   const ColRead cr(lane);
   const uint32_t ring_addr = lds_addr(&lds.ring[0][0][0]);
   const float c2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);  // (not 0, which would make NaN of the masked scores' -inf)
   const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale turns the queries around, so that maxima stay maxima
+  const int kvh = head / a.group;
+  const int len = ti.len, row0 = ti.row0, w0 = row0 + 32 * wave;
+  const uint16_t* kbase = a.k + (int64_t)ti.r0 * a.k_stride + kvh * D;
+  const uint16_t* vbase = a.v + (int64_t)ti.r0 * a.v_stride + kvh * D;
+  const int keys = min(len, row0 + kTileRows), n = (keys + BK - 1) / BK;
+  const int mine = w0 < len ? w0 / BK + 1 : 0;  // blocks this wavefront's queries see
+  auto request = [&](int kt, int stage) {
+    const uint32_t at = ring_addr + stage * (2 * kHalfBytes);
+    dma_block<D, BK>(kbase, a.k_stride, kt * BK, len - 1, wave, at);
+    dma_block<D, BK>(vbase, a.v_stride, kt * BK, len - 1, wave, at + kHalfBytes);
+  };
+  request(0, 0);
 
+  u32x4 qb[NT];  // Q^T as operand: column = query ln, slots = channels 16 t + 8 g .. +7
+  {
+    const uint16_t* qp = a.q + (int64_t)(ti.r0 + min(w0 + ln, len - 1)) * a.q_stride + head * D + 8 * g;
+#pragma unroll
+    for (int t = 0; t < NT; t++) qb[t] = *reinterpret_cast<const u32x4*>(qp + 16 * t);
+#pragma unroll
+    for (int t = 0; t < NT; t++) qb[t] ^= u32x4{sign, sign, sign, sign};
+    // (consumed here, so that the wait for these loads does not stand inside the loop)
+#pragma unroll
+    for (int t = 0; t < NT; t++) asm volatile("" ::"v"(qb[t]));
+  }
+  f32x16 o[NC];
+#pragma unroll
+  for (int cb = 0; cb < NC; cb++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) o[cb][r] = 0.f;
+  float m = -INFINITY, l = 0.f;
+
+  int stage = 0;
+  for (int kt = 0; kt < n; kt++) {
+    wait_vmem<0>();
+    __syncthreads();  // everyone's pieces have landed, and everyone is done with the stage that is requested next
+    if (kt + 1 < n) request(kt + 1, 1 - stage);
+    if (kt < mine) {
+      const uint16_t *sK = &lds.ring[stage][0][0], *sV = &lds.ring[stage][1][0];
+      f32x16 s[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; kb++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) s[kb][r] = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; kb++)
+#pragma unroll
+        for (int t = 0; t < NT; t++) s[kb] = Op<T>::mfma(read_rows<D, BK>(rr, sK, kb, t), qb[t], s[kb]);
+      if (kt * BK + BK - 1 > w0) {  // keys behind some query
+        const int le = lane_id(), room = w0 + (le & 31) - kt * BK - 4 * (le >> 5);  // register r of half kb is masked iff 32 kb + 8 (r / 4) + r % 4 > room
+#pragma unroll
+        for (int kb = 0; kb < KB; kb++)
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (32 * kb + 8 * (r >> 2) + (r & 3) > room) s[kb][r] = -INFINITY;
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; kb++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) top = fmaxf(top, s[kb][r]);
+      top = pair_max(top) * c2;
+      if (__ballot(top > m + 8.f)) {
+        const float up = top > m + 8.f ? top : m;  // (each query by itself: its results are a matter of its own scores)
+        const float keep = m == up ? 1.f : fast_exp2(m - up);
+        m = up;
+        l *= keep;
+#pragma unroll
+        for (int cb = 0; cb < NC; cb++) o[cb] *= keep;
+      }
+      u32x4 pb[2 * KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; kb++) {
+        float p[16];
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          p[r] = fast_exp2(__builtin_fmaf(s[kb][r], c2, -m));
+          l += p[r];
+        }
+#pragma unroll
+        for (int t2 = 0; t2 < 2; t2++)
+          pb[2 * kb + t2] = u32x4{Op<T>::pack2(p[8 * t2], p[8 * t2 + 1]), Op<T>::pack2(p[8 * t2 + 2], p[8 * t2 + 3]),
+                                  Op<T>::pack2(p[8 * t2 + 4], p[8 * t2 + 5]), Op<T>::pack2(p[8 * t2 + 6], p[8 * t2 + 7])};
+      }
+#pragma unroll
+      for (int t2 = 0; t2 < 2 * KB; t2++)
+#pragma unroll
+        for (int cb = 0; cb < NC; cb++) o[cb] = Op<T>::mfma(read_cols<D, BK>(cr, sV, t2, cb), pb[t2], o[cb]);
+    }
+    stage = 1 - stage;
+  }
+  __syncthreads();  // the ring is free: scratch for the rows on their way out
+  if (mine) {
+    l = pair_sum(l);
+    const float inv = 1.f / l;
+    const int le = lane_id();
+    if (le < 32 && w0 + le < len) a.lse[(int64_t)head * a.total + ti.r0 + w0 + le] = (m + __log2f(l)) * kLn2;
+#pragma unroll
+    for (int cb = 0; cb < NC; cb++) o[cb] *= inv;
+    uint16_t* scratch = &lds.ring[0][0][0] + 2048 * wave;
+#pragma unroll
+    for (int h = 0; h < D / 64; h++) {
+      const f32x16 x[2] = {o[2 * h], o[2 * h + 1]};
+      store_rows32<T>(x, 1.f, scratch, a.o, (int64_t)(ti.r0 + w0) * a.o_stride + head * D + 64 * h, a.o_stride, len - w0);
+    }
+  }
+  __syncthreads();
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void causal_fwd_kernel(const CausalArgs a) {
+  __shared__ __align__(1024) CausalFwdLds<D, kFwdKeys<D>> lds;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (int item = blockIdx.x;; item += gridDim.x) {
-    const int rank = item / a.heads;
-    const TileItem ti = causal_tile(a, rank);
-    if (ti.len == 0) return;
-    const int head = causal_head(item - rank * a.heads, a.heads, a.kv_heads, a.group), kvh = head / a.group;
-    const int len = ti.len, row0 = ti.row0, w0 = row0 + 32 * wave;
-    const uint16_t* kbase = a.k + (int64_t)ti.r0 * a.k_stride + kvh * D;
-    const uint16_t* vbase = a.v + (int64_t)ti.r0 * a.v_stride + kvh * D;
-    const int keys = min(len, row0 + kTileRows), n = (keys + kCausalKeys - 1) / kCausalKeys;
-    const int mine = w0 < len ? w0 / kCausalKeys + 1 : 0;  // blocks this wavefront's queries see
-    auto request = [&](int kt, int stage) {
-      const uint32_t at = ring_addr + stage * (2 * kHalfBytes);
-      dma_block<D, kCausalKeys>(kbase, a.k_stride, kt * kCausalKeys, len - 1, wave, at);
-      dma_block<D, kCausalKeys>(vbase, a.v_stride, kt * kCausalKeys, len - 1, wave, at + kHalfBytes);
-    };
-    request(0, 0);
-    if (NST == 3 && n > 1) request(1, 1);
-
-    u32x4 qb[NT];  // Q^T as operand: column = query ln, slots = channels 16 t + 8 g .. +7
-    {
-      const uint16_t* qp = a.q + (int64_t)(ti.r0 + min(w0 + ln, len - 1)) * a.q_stride + head * D + 8 * g;
-#pragma unroll
-      for (int t = 0; t < NT; t++) qb[t] = *reinterpret_cast<const u32x4*>(qp + 16 * t);
-#pragma unroll
-      for (int t = 0; t < NT; t++) qb[t] ^= u32x4{sign, sign, sign, sign};
-      // (consumed here, so that the wait for these loads does not stand inside the loop)
-#pragma unroll
-      for (int t = 0; t < NT; t++) asm volatile("" ::"v"(qb[t]));
+    const int rank = item / a.heads, head = causal_head(item - rank * a.heads, a.heads, a.kv_heads, a.group);
+    TileItem ti;
+    if (a.whole) {
+      if (rank >= a.batch) return;
+      causal_sequence(a, rank, ti.r0, ti.len);
+      ti.row0 = (ti.len - 1) / kTileRows * kTileRows;
+      if (ti.len == 0) continue;
+    } else {
+      ti = causal_tile(a, rank);
+      if (ti.len == 0) return;
     }
-    f32x16 o[NC];
-#pragma unroll
-    for (int cb = 0; cb < NC; cb++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) o[cb][r] = 0.f;
-    float m = -INFINITY, l = 0.f;
-
-    int stage = 0;
-    for (int kt = 0; kt < n; kt++) {
-      if (NST == 3 && kt + 1 < n)
-        wait_vmem<kPieces>();
-      else
-        wait_vmem<0>();
-      __syncthreads();  // everyone's pieces have landed, and everyone is done with the stage that is requested next
-      const int ahead = NST == 3 ? (stage == 0 ? 2 : stage - 1) : 1 - stage;
-      if (kt + NST - 1 < n) request(kt + NST - 1, ahead);
-      if (kt < mine) {
-        const uint16_t *sK = &lds.ring[stage][0][0], *sV = &lds.ring[stage][1][0];
-        f32x16 s[2];
-#pragma unroll
-        for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-          for (int r = 0; r < 16; r++) s[kb][r] = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-          for (int t = 0; t < NT; t++) s[kb] = Op<T>::mfma(read_rows<D, kCausalKeys>(rr, sK, kb, t), qb[t], s[kb]);
-        if (kt * kCausalKeys + kCausalKeys - 1 > w0) {  // keys behind some query
-          const int room = w0 + ln - kt * kCausalKeys - 4 * g;  // register r of half kb is masked iff 32 kb + 8 (r / 4) + r % 4 > room
-#pragma unroll
-          for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-            for (int r = 0; r < 16; r++)
-              if (32 * kb + 8 * (r >> 2) + (r & 3) > room) s[kb][r] = -INFINITY;
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-          for (int r = 0; r < 16; r++) top = fmaxf(top, s[kb][r]);
-        top = fmaxf(top, other_half(top)) * c2;
-        if (__ballot(top > m + 8.f)) {
-          const float up = top > m + 8.f ? top : m;  // (each query by itself: its results are a matter of its own scores)
-          const float keep = m == up ? 1.f : fast_exp2(m - up);
-          m = up;
-          l *= keep;
-#pragma unroll
-          for (int cb = 0; cb < NC; cb++) o[cb] *= keep;
-        }
-        u32x4 pb[4];
-#pragma unroll
-        for (int kb = 0; kb < 2; kb++) {
-          float p[16];
-#pragma unroll
-          for (int r = 0; r < 16; r++) {
-            p[r] = fast_exp2(__builtin_fmaf(s[kb][r], c2, -m));
-            l += p[r];
-          }
-#pragma unroll
-          for (int t2 = 0; t2 < 2; t2++)
-            pb[2 * kb + t2] = u32x4{Op<T>::pack2(p[8 * t2], p[8 * t2 + 1]), Op<T>::pack2(p[8 * t2 + 2], p[8 * t2 + 3]),
-                                    Op<T>::pack2(p[8 * t2 + 4], p[8 * t2 + 5]), Op<T>::pack2(p[8 * t2 + 6], p[8 * t2 + 7])};
-        }
-#pragma unroll
-        for (int t2 = 0; t2 < 4; t2++)
-#pragma unroll
-          for (int cb = 0; cb < NC; cb++) o[cb] = Op<T>::mfma(read_cols<D, kCausalKeys>(cr, sV, t2, cb), pb[t2], o[cb]);
-      }
-      stage = NST == 3 ? (stage == 2 ? 0 : stage + 1) : 1 - stage;
-    }
-    __syncthreads();  // the ring is free: scratch for the rows on their way out
-    if (mine) {
-      l += other_half(l);
-      const float inv = 1.f / l;
-      if (lane < 32 && w0 + ln < len) a.lse[(int64_t)head * a.total + ti.r0 + w0 + ln] = (m + __log2f(l)) * kLn2;
-#pragma unroll
-      for (int cb = 0; cb < NC; cb++) o[cb] *= inv;
-      uint16_t* scratch = &lds.ring[0][0][0] + 2048 * wave;
-#pragma unroll
-      for (int h = 0; h < D / 64; h++) {
-        const f32x16 x[2] = {o[2 * h], o[2 * h + 1]};
-        store_rows32<T>(x, 1.f, scratch, a.o, (int64_t)(ti.r0 + w0) * a.o_stride + head * D + 64 * h, a.o_stride, len - w0);
-      }
-    }
-    __syncthreads();
+    do {
+      causal_fwd_tile<T, D>(a, lds, ti, head, wave);
+      ti.row0 -= kTileRows;
+    } while (a.whole && ti.row0 >= 0);
   }
 }
 
