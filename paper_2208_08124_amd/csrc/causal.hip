@@ -21,14 +21,14 @@ int64_t tile_capacity(int64_t batch, int64_t total) { return total / fmha::kTile
 
 // The dK/dV pass: its items are key tiles by key heads, of steps = group x (blocks of 32 queries from the diagonal on).
 // Where the longest item has much more than a workgroup's share of all steps (of 512 that run at a time), the chip would wait for
-// it, and items are cut into parts of at least 16 steps.  The share is estimated from below, by sequences that are all as long.
+// it, and items are cut into parts of at least 8 steps (16 x up to 256, 12 / 4 heads of 64: 42 us by parts of 16, 36 by 8).  The share is estimated from below, by sequences that are all as long.
 // Cutting costs the parts' sums on their way through memory.  Backward, us, whole / cut (in how many), head size 128:
 //   1 x 16384, 16 / 2 heads    longest 4.0 shares   8000 / 5276 (4), 4399 (8), 3888 (16)
 //   6 x up to 4096, 32 / 8     1.9                  1488 / 1472 (3), 1430 (5)
 //   12 x up to 4000, 32 / 8    1.3                  2028 / 2216 (2)
 //   1 x 16384, 32 / 8          1.0                  7084 / 7265 (4)
 //   64 x 512, 16 / 4           1.0                   403 / 458 (2), 604 (4)
-constexpr int64_t kPartsMost = 16, kPartSteps = 16, kPartBytes = (int64_t)512 << 20;
+constexpr int64_t kPartsMost = 16, kPartSteps = 8, kPartBytes = (int64_t)512 << 20;
 int64_t steps_of(int64_t len, int64_t group) { return (len + fmha::kCausalQueries - 1) / fmha::kCausalQueries * group; }
 int64_t parts_for(int64_t batch, int64_t total, int64_t group, int64_t kv_heads, int64_t longest) {
   if (batch <= 0 || total <= 0 || steps_of(longest, group) <= kPartSteps) return 1;

@@ -167,7 +167,7 @@ __device__ __forceinline__ void qk_gamma(float (&w)[16], const float* __restrict
   }
 }
 
-// Row and position of the lane's token: tokens tok0 .. tok0 + tpw - 1 belong to the wavefront, the lane to number `mine`.
+// Position of the lane's token: tokens tok0 .. tok0 + tpw - 1 belong to the wavefront, the lane to number `mine`.
 // CACHE: also the sequence.
 template <bool CACHE>
 __device__ __forceinline__ int qk_position(const QkRows& a, int tok0, int tpw, int mine, int present, int& seq) {
@@ -181,11 +181,24 @@ __device__ __forceinline__ int qk_position(const QkRows& a, int tok0, int tpw, i
     }
     return pos;
   }
+  const int lane = threadIdx.x & 63;
+  int begin = 0, end = 0x7fffffff, held = 0;  // of sequence `lane`, where each has a lane
+  if (a.batch <= 64 && lane < a.batch) {
+    begin = a.cu[lane];
+    end = a.cu[lane + 1];
+    if (CACHE) held = a.seqlens[lane];
+  }
   for (int i = 0; i < tpw; i++) {
     const int t = tok0 + i;
     if (t >= present) break;
-    const int s = qk_sequence(a.cu, a.batch, t);
-    const int at = CACHE ? a.seqlens[s] - a.cu[s + 1] + t : t - a.cu[s];
+    int s, at;
+    if (a.batch <= 64) {
+      s = min((int)__popcll(__ballot(end <= t)), a.batch - 1);
+      at = CACHE ? __builtin_amdgcn_readlane(held, s) - __builtin_amdgcn_readlane(end, s) + t : t - __builtin_amdgcn_readlane(begin, s);
+    } else {
+      s = qk_sequence(a.cu, a.batch, t);
+      at = CACHE ? a.seqlens[s] - a.cu[s + 1] + t : t - a.cu[s];
+    }
     if (i == mine) {
       pos = at;
       seq = s;
@@ -208,11 +221,25 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_kernel(const QkRows a) {
   const int part = (int)(wave - group * a.parts);
   const int c = lane % a.lp2, slot = lane / a.lp2;
   const int mine = slot / a.gs, tok = tok0 + mine;
+  const bool on = c < a.lph;  // not one of the lanes that a head is padded with
+  const QkPieces pc = QkPieces::of<INTER>(c, a.lph, a.rot);
+  const int heads = a.nq + a.nk + a.nv;
+  const int first = part * a.iters * a.gs + slot % a.gs, last = min(heads, first + a.iters * a.gs);
+  auto fetch = [&](u32x4& w1, u32x4& w2, int h) {
+    w1 = w2 = u32x4{0u, 0u, 0u, 0u};
+    if (!on || tok >= present || h >= last) return;
+    const bool is_v = CACHE && h >= a.nq + a.nk;
+    const uint16_t* src = h < a.nq ? a.q + tok * a.q_stride + (int64_t)h * a.dim
+                          : is_v   ? a.v + tok * a.v_stride + (int64_t)(h - a.nq - a.nk) * a.dim
+                                   : a.k + tok * a.k_stride + (int64_t)(h - a.nq) * a.dim;
+    w1 = *reinterpret_cast<const u32x4*>(src + 8 * pc.one);
+    w2 = *reinterpret_cast<const u32x4*>(src + 8 * pc.two);
+  };
+  u32x4 w1, w2;
+  fetch(w1, w2, first);  // (ahead of all that it takes to know the position)
   int seq;
   const int pos = a.rot || CACHE ? qk_position<CACHE>(a, tok0, tpw, mine, present, seq) : 0;
-  if (tok >= present) return;  // (here and below control goes by whole heads: what their lanes exchange is there)
-  const bool on = c < a.lph;   // not one of the lanes that a head is padded with
-  const QkPieces pc = QkPieces::of<INTER>(c, a.lph, a.rot);
+  if (tok >= present || first >= last) return;  // (here and below control goes by whole heads: what their lanes exchange is there)
   int64_t place = -1;  // of the token in a cache of one head
   if (CACHE) {
     const int page = pos >> a.page_shift;
@@ -222,32 +249,20 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_kernel(const QkRows a) {
         place = g * a.page_stride + (int64_t)(pos & ((1 << a.page_shift) - 1)) * a.dim;
     }
   }
-  const int heads = a.nq + a.nk + a.nv;
-  const int first = part * a.iters * a.gs + slot % a.gs;
-  if (first >= heads) return;
   float cs[8], sn[8];
   if (on) qk_angles<INTER>(cs, sn, pc, a.inv_freq, pos, a.magnitude);
-  for (int it = 0; it < a.iters; it++) {
-    const int h = first + it * a.gs;
-    if (h >= heads) break;
+  for (int h = first; h < last; h += a.gs) {
+    u32x4 next1, next2;
+    fetch(next1, next2, h + a.gs);
     const bool is_q = h < a.nq, is_v = CACHE && h >= a.nq + a.nk;
     const int hk = h - a.nq - (is_v ? a.nk : 0);
-    const uint16_t* src = is_q ? a.q + tok * a.q_stride + (int64_t)h * a.dim
-                               : (is_v ? a.v + tok * a.v_stride : a.k + tok * a.k_stride) + (int64_t)hk * a.dim;
-    uint16_t* dst;
-    if (is_q) {
+    uint16_t* dst = nullptr;  // (null: a token without a place)
+    if (is_q)
       dst = a.qo + tok * a.qo_stride + (int64_t)h * a.dim;
-    } else if (CACHE) {
-      if (place < 0) continue;
-      dst = (is_v ? a.vc : a.kc) + place + (((int64_t)hk * a.dim) << a.page_shift);
-    } else {
+    else if (!CACHE)
       dst = a.ko + tok * a.ko_stride + (int64_t)hk * a.dim;
-    }
-    u32x4 w1 = {0u, 0u, 0u, 0u}, w2 = w1;
-    if (on) {
-      w1 = *reinterpret_cast<const u32x4*>(src + 8 * pc.one);
-      w2 = *reinterpret_cast<const u32x4*>(src + 8 * pc.two);
-    }
+    else if (place >= 0)
+      dst = (is_v ? a.vc : a.kc) + place + (((int64_t)hk * a.dim) << a.page_shift);
     if (!is_v) {
       float x[16];
       qk_unpack<T>(x, w1, w2);
@@ -262,13 +277,15 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_kernel(const QkRows a) {
 #pragma unroll
         for (int j = 0; j < 16; j++) x[j] *= rstd * w[j];
       }
-      qk_turn<INTER, false>(x, cs, sn, pc);
+      if (on) qk_turn<INTER, false>(x, cs, sn, pc);
       qk_pack<T>(w1, w2, x);
     }
-    if (on) {
+    if (on && dst) {
       *reinterpret_cast<u32x4*>(dst + 8 * pc.one) = w1;
       *reinterpret_cast<u32x4*>(dst + 8 * pc.two) = w2;
     }
+    w1 = next1;
+    w2 = next2;
   }
 }
 
@@ -276,7 +293,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_kernel(const QkRows a) {
 // then added up over the wavefront's heads and rows, over the workgroup, and by qk_gamma_kernel over the
 // workgroups, always in the same order.  partial: [workgroups][2][dim].
 template <typename T, bool INTER>
-__global__ __launch_bounds__(kQkThreads) void qk_rows_bwd_kernel(const QkRows a) {
+__global__ __launch_bounds__(kQkThreads, 3) void qk_rows_bwd_kernel(const QkRows a) {
   __shared__ float sums[kQkThreads / 64][2][256];  // (first gamma: [0][0] of the queries, [0][1] of the keys)
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int slots = 64 / a.lp2, tpw = slots / a.gs;
@@ -285,7 +302,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_bwd_kernel(const QkRows a)
   const bool on = c < a.lph;
   const QkPieces pc = QkPieces::of<INTER>(c, a.lph, a.rot);
   const int heads = a.nq + a.nk;
-  const int groups = (present + tpw - 1) / tpw;
+  const int items = (present + tpw - 1) / tpw * a.parts;
   for (int i = threadIdx.x; i < a.dim; i += kQkThreads) {
     sums[0][0][i] = a.gamma_q ? a.gamma_q[i] : 1.f;
     sums[0][1][i] = a.gamma_k ? a.gamma_k[i] : 1.f;
@@ -295,9 +312,9 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_bwd_kernel(const QkRows a)
     u32x4 g1, g2, x1, x2;
   };
   // (an empty place, or a lane that its head is padded with, works on zeros)
-  auto fetch = [&](Raw& r, int tok, int h) {
+  auto fetch = [&](Raw& r, int tok, int h, int last) {
     r.g1 = r.g2 = r.x1 = r.x2 = u32x4{0u, 0u, 0u, 0u};
-    if (!on || h >= heads || tok >= present) return;
+    if (!on || h >= last || tok >= present) return;
     const bool is_q = h < a.nq;
     const int64_t col = (int64_t)(is_q ? h : h - a.nq) * a.dim;
     const uint16_t* dy = is_q ? a.dyq + tok * a.qo_stride + col : a.dyk + tok * a.ko_stride + col;
@@ -310,18 +327,20 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_bwd_kernel(const QkRows a)
     }
   };
   float sum_q[16] = {}, sum_k[16] = {};
-  for (int group = blockIdx.x * (kQkThreads / 64) + w; group < groups; group += gridDim.x * (kQkThreads / 64)) {
+  for (int item = blockIdx.x * (kQkThreads / 64) + w; item < items; item += gridDim.x * (kQkThreads / 64)) {
+    const int group = item / a.parts, part = item - group * a.parts;
     const int tok0 = __builtin_amdgcn_readfirstlane(group * tpw), tok = tok0 + mine;
+    const int first = part * a.iters * a.gs + slot % a.gs, last = min(heads, first + a.iters * a.gs);
     Raw cur;
-    fetch(cur, tok, slot % a.gs);
+    fetch(cur, tok, first, last);
     int seq;
     const int pos = a.rot ? qk_position<false>(a, tok0, tpw, mine, present, seq) : 0;
     if (tok >= present) continue;  // (whole heads)
     float cs[8], sn[8];
     if (on) qk_angles<INTER>(cs, sn, pc, a.inv_freq, pos, a.magnitude);
-    for (int h = slot % a.gs; h < heads; h += a.gs) {
+    for (int h = first; h < last; h += a.gs) {
       Raw next;
-      fetch(next, tok, h + a.gs);  // the next head's rows, ahead of this one's work
+      fetch(next, tok, h + a.gs, last);  // the next head's rows, ahead of this one's work
       const bool is_q = h < a.nq;
       const bool normed = is_q ? a.gamma_q : a.gamma_k;
       float g[16];
