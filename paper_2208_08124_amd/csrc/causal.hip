@@ -165,23 +165,23 @@ int launch_list(const fmha_causal_params_t* p, const fmha::CausalArgs& a, bool n
   return FMHA_OK;
 }
 
-// Workgroups for a pass over the tiles of `heads` heads, and the order in which it takes them.
-unsigned plan(const fmha_causal_params_t* p, int heads, fmha::CausalArgs* a) {
-  const unsigned grid = grid_of(p, heads);
-  a->by_cost = grid <= kByCost;
+// Workgroups for a pass over the tiles of `heads` heads in up to `parts` parts each, and the order in which it takes them.
+unsigned plan(const fmha_causal_params_t* p, int heads, int parts, fmha::CausalArgs* a) {
+  const unsigned items = grid_of(p, heads);
+  a->by_cost = items <= kByCost;
   if (p->batch > fmha::kCausalSelf) {
     const Workspace w = carve(p->batch, p->total_tokens, p->heads, p->kv_heads, p->head_dim);
     char* base = static_cast<char*>(p->workspace);
     a->count = reinterpret_cast<int32_t*>(base);
     a->list = reinterpret_cast<fmha::TileItem*>(base + (a->by_cost ? w.by_cost : w.by_sequence));
   }
-  return grid;
+  return items * (unsigned)parts;
 }
 
 template <typename T, int D>
 int launch_fwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st) {
   a.whole = whole(p);
-  const unsigned grid = a.whole ? (unsigned)(p->batch * a.heads) : plan(p, a.heads, &a);
+  const unsigned grid = a.whole ? (unsigned)(p->batch * a.heads) : plan(p, a.heads, 1, &a);
   fmha::causal_fwd_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal forward launch failed: %s", hipGetErrorString(e));
@@ -196,11 +196,11 @@ int launch_bwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st
     if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal backward launch failed: %s", hipGetErrorString(e));
     return FMHA_OK;
   }
-  unsigned grid = plan(p, a.heads, &a);
+  unsigned grid = plan(p, a.heads, 1, &a);
   fmha::causal_dq_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal dQ launch failed: %s", hipGetErrorString(e));
-  grid = plan(p, a.kv_heads * a.parts, &a);
+  grid = plan(p, a.kv_heads, a.parts, &a);
   fmha::causal_dkv_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal dK/dV launch failed: %s", hipGetErrorString(e));
