@@ -118,8 +118,8 @@ int fmha_cache_attention(const fmha_cache_t* c, int32_t heads, int32_t max_seqle
   a.splits = s.splits;
   a.waves = s.waves;
   a.scale = scale;
-  a.part_o = static_cast<float*>(workspace);
-  a.part_lse = a.part_o + (size_t)s.splits * (size_t)c->batch * (size_t)heads * (size_t)c->head_dim;
+  if (need) a.part_o = static_cast<float*>(workspace);
+  if (need) a.part_lse = a.part_o + (size_t)s.splits * (size_t)c->batch * (size_t)heads * (size_t)c->head_dim;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (c->dtype == FMHA_F16) return c->head_dim == 64 ? launch<_Float16, 64>(a, st) : launch<_Float16, 128>(a, st);
   return c->head_dim == 64 ? launch<__bf16, 64>(a, st) : launch<__bf16, 128>(a, st);
