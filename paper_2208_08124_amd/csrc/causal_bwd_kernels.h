@@ -176,13 +176,13 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 2) void causal_dq_kernel(co
 }
 
 // ------------------------------------------------------------------ dK, dV
-// Queries go by in blocks of 32.  The wavefront's 32 keys: V as operand in registers, K too at 64 channels; at 128 the
-// accumulators leave no room for it and K is read from LDS.
+// Queries go by in blocks of 32.  The wavefront's 32 keys stand in registers as operands, V and the last 64 channels of K; at 128
+// channels the accumulators leave no room for the first 64 of K, which are read from LDS (all of it from there: 1 % slower).
 constexpr int kCausalQueries = 32;
 
 template <int D>
 struct CausalDkvLds {
-  uint16_t k[D == 64 ? 8 : kTileRows * D];  // [64-row half][..]
+  uint16_t k[D == 64 ? 8 : kTileRows * 64];  // channels 0 .. 63: two tiles of 64 rows
   struct alignas(1024) {
     uint16_t q[kCausalQueries * D], g[kCausalQueries * D];
     float stat[4][64];  // per wavefront: lse log2(e) of the 32 queries, then -D of them
@@ -230,11 +230,11 @@ __device__ __forceinline__ void causal_dkv_tile(const CausalArgs& a, CausalDkvLd
   if (D == 128) {
     const uint16_t* kbase = a.k + (int64_t)ti.r0 * a.k_stride + kvh * D;
     // two blocks of 64 rows; rows behind the end repeat the last one
-    dma_block<D, 64>(kbase, a.k_stride, k0, len - 1, wave, lds_addr(&lds.k[0]));
-    if (k0 + 64 < len) dma_block<D, 64>(kbase, a.k_stride, k0 + 64, len - 1, wave, lds_addr(&lds.k[0]) + 64 * D * 2);
+    dma_block<64, 64>(kbase, a.k_stride, k0, len - 1, wave, lds_addr(&lds.k[0]));
+    if (k0 + 64 < len) dma_block<64, 64>(kbase, a.k_stride, k0 + 64, len - 1, wave, lds_addr(&lds.k[0]) + 64 * 64 * 2);
   }
   request(0);
-  u32x4 kb4[D == 64 ? NT : 1], vb[NT];
+  u32x4 kb4[4], vb[NT];
   {
     const int64_t tok = ti.r0 + min(w0 + ln, len - 1);
     const uint16_t* kp = a.k + tok * a.k_stride + kvh * D + 8 * g;
@@ -242,12 +242,12 @@ __device__ __forceinline__ void causal_dkv_tile(const CausalArgs& a, CausalDkvLd
 #pragma unroll
     for (int t = 0; t < NT; t++) {
       vb[t] = *reinterpret_cast<const u32x4*>(vp + 16 * t);
-      if (D == 64) kb4[t] = *reinterpret_cast<const u32x4*>(kp + 16 * t);
+      if (t >= NT - 4) kb4[t & 3] = *reinterpret_cast<const u32x4*>(kp + 16 * t);
     }
 #pragma unroll
     for (int t = 0; t < NT; t++) {
       asm volatile("" ::"v"(vb[t]));
-      if (D == 64) asm volatile("" ::"v"(kb4[t]));
+      if (t < 4) asm volatile("" ::"v"(kb4[t & 3]));
     }
   }
   f32x16 dk[NC], dv[NC];
@@ -255,7 +255,7 @@ __device__ __forceinline__ void causal_dkv_tile(const CausalArgs& a, CausalDkvLd
   for (int cb = 0; cb < NC; cb++)
 #pragma unroll
     for (int r = 0; r < 16; r++) dk[cb][r] = dv[cb][r] = 0.f;
-  const uint16_t* myk = &lds.k[0] + (wave >> 1) * (64 * D);
+  const uint16_t* myk = &lds.k[0] + (wave >> 1) * (64 * 64);
 
   int stage = 0;
   for (int i = 0; i < n; i++) {
@@ -274,7 +274,7 @@ __device__ __forceinline__ void causal_dkv_tile(const CausalArgs& a, CausalDkvLd
       for (int r = 0; r < 16; r++) s[r] = dp[r] = 0.f;
 #pragma unroll
       for (int t = 0; t < NT; t++) {
-        const u32x4 kk = D == 64 ? kb4[D == 64 ? t : 0] : read_rows<D, 64>(rr, myk, wave & 1, t);
+        const u32x4 kk = t >= NT - 4 ? kb4[t & 3] : rr.read(myk, wave & 1, t & 3);
         s = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.q, 0, t), kk, s);
         dp = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.g, 0, t), vb[t], dp);
       }
