@@ -77,11 +77,11 @@ __device__ __forceinline__ void causal_dq_tile(const CausalArgs& a, CausalFwdLds
     const uint16_t *sK = &lds.ring[kt & 1][0][0], *sV = &lds.ring[kt & 1][1][0];
 #pragma unroll
     for (int r = 0; r < 16; r++) s[r] = dp[r] = 0.f;
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-      s = Op<T>::mfma(read_rows<D, kCausalKeys>(rr, sK, kb, t), qb[t], s);
-      dp = Op<T>::mfma(read_rows<D, kCausalKeys>(rr, sV, kb, t), gb[t], dp);
-    }
+    products<2 * NT, kAhead<D>>([&](int i) { return read_rows<D, kCausalKeys>(rr, i & 1 ? sV : sK, kb, i / 2); })
+        .run([&](int i, const u32x4& x) {
+          if (i & 1) dp = Op<T>::mfma(x, gb[i / 2], dp);
+          else s = Op<T>::mfma(x, qb[i / 2], s);
+        });
   };
   // rowsum(dO o O) carries the rounding of the stored O, which tells where few keys share a row: a row of n keys has an O, and
   // with it that error, of about 1 / sqrt(n) of a V.  The first tile's rows take D = rowsum(P o dP), which is the same without it,
@@ -119,6 +119,7 @@ __device__ __forceinline__ void causal_dq_tile(const CausalArgs& a, CausalFwdLds
         if (key0 > w0) break;  // (blocks of 32 line up with the wavefronts' queries)
         f32x16 s, dp;
         scores(kt, kb, s, dp);
+        auto dsk = products<2 * NC, kAhead<D>>([&](int i) { return read_cols<D, kCausalKeys>(cr, sK, 2 * kb + i / NC, i % NC); });
         float ds[16];
 #pragma unroll
         for (int r = 0; r < 16; r++) ds[r] = fast_exp2(__builtin_fmaf(s[r], c2, -lse2)) * (dp[r] - dsum);
@@ -129,10 +130,7 @@ __device__ __forceinline__ void causal_dq_tile(const CausalArgs& a, CausalFwdLds
             if (8 * (r >> 2) + (r & 3) > room) ds[r] = 0.f;
         }
         const u32x4 dsb[2] = {pack_half<T>(ds, 0), pack_half<T>(ds, 1)};
-#pragma unroll
-        for (int t2 = 0; t2 < 2; t2++)
-#pragma unroll
-          for (int cb = 0; cb < NC; cb++) dq[cb] = Op<T>::mfma(read_cols<D, kCausalKeys>(cr, sK, 2 * kb + t2, cb), dsb[t2], dq[cb]);
+        dsk.run([&](int i, const u32x4& x) { dq[i % NC] = Op<T>::mfma(x, dsb[i / NC], dq[i % NC]); });
       }
     }
   }
@@ -272,12 +270,20 @@ __device__ __forceinline__ void causal_dkv_tile(const CausalArgs& a, CausalDkvLd
       f32x16 s, dp;
 #pragma unroll
       for (int r = 0; r < 16; r++) s[r] = dp[r] = 0.f;
-#pragma unroll
-      for (int t = 0; t < NT; t++) {
-        const u32x4 kk = t >= NT - 4 ? kb4[t & 3] : rr.read(myk, wave & 1, t & 3);
-        s = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.q, 0, t), kk, s);
-        dp = Op<T>::mfma(read_rows<D, kCausalQueries>(rr, st.g, 0, t), vb[t], dp);
+      products<NT, kAhead<D>>([&](int i) { return read_rows<D, kCausalQueries>(rr, st.g, 0, i); }).run([&](int i, const u32x4& x) {
+        dp = Op<T>::mfma(x, vb[i], dp);
+      });
+      if (D == 128) {
+        u32x4 kk;
+        products<8, 2>([&](int i) { return i & 1 ? read_rows<D, kCausalQueries>(rr, st.q, 0, i / 2) : rr.read(myk, wave & 1, i / 2); })
+            .run([&](int i, const u32x4& x) {
+              if (i & 1) s = Op<T>::mfma(x, kk, s);
+              else kk = x;
+            });
       }
+      products<4, kAhead<D>>([&](int i) { return read_rows<D, kCausalQueries>(rr, st.q, 0, NT - 4 + i); }).run([&](int i, const u32x4& x) {
+        s = Op<T>::mfma(x, kb4[i], s);
+      });
       float p[16], ds[16];
 #pragma unroll
       for (int j = 0; j < 4; j++) {
@@ -297,13 +303,12 @@ __device__ __forceinline__ void causal_dkv_tile(const CausalArgs& a, CausalDkvLd
           if (8 * (r >> 2) + (r & 3) < room) p[r] = ds[r] = 0.f;
       }
       const u32x4 pb[2] = {pack_half<T>(p, 0), pack_half<T>(p, 1)}, dsb[2] = {pack_half<T>(ds, 0), pack_half<T>(ds, 1)};
-#pragma unroll
-      for (int t2 = 0; t2 < 2; t2++)
-#pragma unroll
-        for (int cb = 0; cb < NC; cb++) {
-          dv[cb] = Op<T>::mfma(read_cols<D, kCausalQueries>(cr, st.g, t2, cb), pb[t2], dv[cb]);
-          dk[cb] = Op<T>::mfma(read_cols<D, kCausalQueries>(cr, st.q, t2, cb), dsb[t2], dk[cb]);
-        }
+      products<4 * NC, kAhead<D>>([&](int i) { return read_cols<D, kCausalQueries>(cr, i & 1 ? st.q : st.g, i / 2 / NC, i / 2 % NC); })
+          .run([&](int i, const u32x4& x) {
+            const int t2 = i / 2 / NC, cb = i / 2 % NC;
+            if (i & 1) dk[cb] = Op<T>::mfma(x, dsb[t2], dk[cb]);
+            else dv[cb] = Op<T>::mfma(x, pb[t2], dv[cb]);
+          });
     }
     stage = 1 - stage;
   }

@@ -33,37 +33,53 @@ __device__ __forceinline__ u32x4 read_cols(const ColRead& cr, const uint16_t* ti
   return cr.read(tile + (cb >> 1) * ROWS * 64, step, cb & 1);
 }
 
-// N products with operands from LDS, B at a time: those of the next B are requested ahead of these B products.  `buf` holds the
-// first B.  (Left to itself the compiler reads each operand right before its product, which then waits for it.  One sequence of 16384,
-// 32 / 8 heads of 128: 1967 us with B = 4, 1966 with 2 or 8, 2012 without; 16 x 2048: 605 and 628.  64 channels hold four workgroups
-// on a compute unit, which hide each other's waits: 191 us with B = 2 and without; 4 takes spills, 199.)
-template <int N, int B, typename Read, typename Use>
-__device__ __forceinline__ void products_from(u32x4 (&buf)[B], Read read, Use use) {
-  static_assert(N % B == 0, "whole batches");
+// N products with operands from LDS: those of the next kAhead products are requested ahead of the kAhead that are under way.  (Left
+// to itself the compiler reads an operand right before its product, which then waits for it.  16384 tokens, 32 / 8 heads of 128:
+// forward 1966 us, 2012 without; backward 6905 us, 7105; 6 x 4096 tokens: backward 1360 us, 1444.  At 64 channels three and four
+// workgroups on a compute unit hide each other's waits, and the registers are full: 16 x 2048 tokens, 16 heads, backward 570 us
+// with, 565 without.)
+template <int D>
+constexpr int kAhead = D == 128 ? 2 : 0;
+
+template <int N, int B, typename Read>
+struct Products {
+  static_assert(B == 0 || N % B == 0, "whole batches");
+  Read read;
+  u32x4 buf[B ? B : 1];
+  __device__ __forceinline__ Products(Read r) : read(r) {  // the first operands are requested here
 #pragma unroll
-  for (int c = 0; c < N; c += B) {
-    u32x4 next[B];
-    __builtin_amdgcn_sched_barrier(0);
-    if (c + B < N) {
+    for (int i = 0; i < B; i++) buf[i] = read(i);
+    if (B) __builtin_amdgcn_sched_barrier(0);
+  }
+  template <typename Use>
+  __device__ __forceinline__ void run(Use use) {
+    if constexpr (B == 0) {
 #pragma unroll
-      for (int i = 0; i < B; i++) next[i] = read(c + B + i);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < N; i++) use(i, read(i));
+    } else {
 #pragma unroll
-    for (int i = 0; i < B; i++) use(c + i, buf[i]);
-    if (c + B < N) {
+      for (int c = 0; c < N; c += B) {
+        u32x4 next[B];
+        __builtin_amdgcn_sched_barrier(0);
+        if (c + B < N) {
 #pragma unroll
-      for (int i = 0; i < B; i++) buf[i] = next[i];
+          for (int i = 0; i < B; i++) next[i] = read(c + B + i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < B; i++) use(c + i, buf[i]);
+        if (c + B < N) {
+#pragma unroll
+          for (int i = 0; i < B; i++) buf[i] = next[i];
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  __builtin_amdgcn_sched_barrier(0);
-}
-template <int N, int B, typename Read, typename Use>
-__device__ __forceinline__ void products(Read read, Use use) {
-  u32x4 buf[B];
-#pragma unroll
-  for (int i = 0; i < B; i++) buf[i] = read(i);
-  products_from<N, B>(buf, read, use);
+};
+template <int N, int B, typename Read>
+__device__ __forceinline__ Products<N, B, Read> products(Read read) {
+  return Products<N, B, Read>(read);
 }
 
 template <typename T, int D>
@@ -119,14 +135,11 @@ __device__ __forceinline__ void causal_fwd_tile(const CausalArgs& a, CausalFwdLd
       for (int kb = 0; kb < KB; kb++)
 #pragma unroll
         for (int r = 0; r < 16; r++) s[kb][r] = 0.f;
-      constexpr int B = D == 128 ? 4 : 2;
-      products<KB * NT, B>([&](int i) { return read_rows<D, BK>(rr, sK, i / NT, i % NT); },
-                           [&](int i, const u32x4& k) { s[i / NT] = Op<T>::mfma(k, qb[i % NT], s[i / NT]); });
-      auto read_v = [&](int i) { return read_cols<D, BK>(cr, sV, i / NC, i % NC); };
-      u32x4 vbuf[B];  // (the first of V's operands come in while the softmax is formed)
-#pragma unroll
-      for (int i = 0; i < B; i++) vbuf[i] = read_v(i);
-      __builtin_amdgcn_sched_barrier(0);
+      products<KB * NT, kAhead<D>>([&](int i) { return read_rows<D, BK>(rr, sK, i / NT, i % NT); }).run([&](int i, const u32x4& k) {
+        s[i / NT] = Op<T>::mfma(k, qb[i % NT], s[i / NT]);
+      });
+      // (the first of V's operands come in while the softmax is formed)
+      auto pv = products<2 * KB * NC, kAhead<D>>([&](int i) { return read_cols<D, BK>(cr, sV, i / NC, i % NC); });
       if (kt * BK + BK - 1 > w0) {  // keys behind some query
         const int le = lane_id(), room = w0 + (le & 31) - kt * BK - 4 * (le >> 5);  // register r of half kb is masked iff 32 kb + 8 (r / 4) + r % 4 > room
 #pragma unroll
@@ -163,7 +176,7 @@ __device__ __forceinline__ void causal_fwd_tile(const CausalArgs& a, CausalFwdLd
           pb[2 * kb + t2] = u32x4{Op<T>::pack2(p[8 * t2], p[8 * t2 + 1]), Op<T>::pack2(p[8 * t2 + 2], p[8 * t2 + 3]),
                                   Op<T>::pack2(p[8 * t2 + 4], p[8 * t2 + 5]), Op<T>::pack2(p[8 * t2 + 6], p[8 * t2 + 7])};
       }
-      products_from<2 * KB * NC, B>(vbuf, read_v, [&](int i, const u32x4& v) { o[i % NC] = Op<T>::mfma(v, pb[i / NC], o[i % NC]); });
+      pv.run([&](int i, const u32x4& v) { o[i % NC] = Op<T>::mfma(v, pb[i / NC], o[i % NC]); });
     }
     stage = 1 - stage;
   }
