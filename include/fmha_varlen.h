@@ -491,9 +491,13 @@ int fmha_cache_attention(const fmha_cache_t* c, int32_t heads, int32_t max_seqle
 /* ---- Causal attention with grouped heads ------------------------------------------
  * As fmha_varlen_fwd / _bwd, but query i of a sequence attends keys 0 .. i of it, and key / value heads are shared:
  *   q, o, d_o, dq : device [T, heads, head_dim];  k, v, dk, dv : device [T, kv_heads, head_dim];  lse : fp32 [heads, T]
- *   dK, dV sum over the query heads that share them, in fp32 and in a fixed order: results repeat bit for bit.
+ *   dK, dV sum over the query heads that share them, in fp32 and in a fixed order: results repeat bit for bit (sizes and
+ *   max_seqlen being the same: they decide in how many parts a long sum is taken, which may move a result by a rounding).
  * Rows at and beyond cu_seqlens[batch] are neither read nor written.  The backward needs the forward's o and lse, and a
- * workspace sized with need_bwd. */
+ * workspace sized with need_bwd (few long sequences: up to 512 MiB more, for sums taken in parts).  Calls that may overlap in
+ * time need workspaces of their own.
+ * An infinity or NaN in a sequence's k, v, q or d_o may reach any of its rows (a masked probability is 0, and 0 * inf is NaN), but no
+ * other sequence's. */
 typedef struct fmha_causal_params {
   int32_t batch;        /* as in fmha_varlen_params_t */
   int32_t total_tokens; /* rows the tensors hold, >= cu_seqlens[batch] */
@@ -502,7 +506,8 @@ typedef struct fmha_causal_params {
   int32_t head_dim;     /* 64 or 128 */
   int32_t max_seqlen;   /* upper bound on the longest sequence, or <= 0 if unknown; a wrong value costs time, not correctness */
   int32_t dtype;        /* fmha_dtype_t */
-  uint32_t flags;       /* FMHA_FLAG_REUSE_SCHEDULE or 0 */
+  uint32_t flags;       /* FMHA_FLAG_REUSE_SCHEDULE (the workspace was last used by a call with the same batch, total_tokens,
+                           max_seqlen and cu_seqlens) or 0 */
   float scale;
   int64_t q_stride, k_stride, v_stride, o_stride;
   int64_t do_stride, dq_stride, dk_stride, dv_stride;

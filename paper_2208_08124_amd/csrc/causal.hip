@@ -126,21 +126,24 @@ int check_common(const fmha_causal_params_t* p, bool bwd, fmha::CausalArgs* a) {
   return FMHA_OK;
 }
 
-// Workgroups for the tiles of `heads` heads: one each, by the sizes that the host knows (the kernels go on in strides, so
+// A launch holds less than 2^32 threads; the kernels go on in strides.
+constexpr int64_t kMostGroups = (int64_t)1 << 23;
+unsigned grid(int64_t groups) { return (unsigned)(groups < kMostGroups ? groups : kMostGroups); }
+
+// Items for the tiles of `heads` heads, by the sizes that the host knows (a workgroup each; the kernels go on in strides, so
 // that a wrong max_seqlen costs time only).
-unsigned grid_of(const fmha_causal_params_t* p, int heads) {
+int64_t items_of(const fmha_causal_params_t* p, int heads) {
   int64_t tiles = tile_capacity(p->batch, p->total_tokens);
   if (p->max_seqlen > 0) {
     const int64_t by_length = ((int64_t)p->max_seqlen + fmha::kTileRows - 1) / fmha::kTileRows * p->batch;
     if (by_length < tiles) tiles = by_length;
   }
-  int64_t g = tiles * heads;
-  return (unsigned)(g < 1 ? 1 : g);
+  return tiles < 1 ? 1 : tiles * heads;
 }
 
 // Items up to which the tiles are taken by cost.  us, by sequence / by cost: 64 x 512 tokens, 16 / 4 heads of 128, backward
 // (1280 items of keys) 465 / 408; 8 x 4096, 32 / 32 heads of 128, forward (8192) 1160 / 1566.
-constexpr unsigned kByCost = 2048;
+constexpr int64_t kByCost = 2048;
 
 // Whether all sequences are (said to be) of one tile: the forward's items are then sequences, and nothing is looked up
 // (256 x 43 .. 128 tokens, 16 heads of 64: 43 us with tiles and their list, 35 so).
@@ -152,8 +155,9 @@ bool whole(const fmha_causal_params_t* p) { return p->max_seqlen > 0 && p->max_s
 // 256 x 43 .. 128, 32 / 8 364 / 386.
 bool whole_bwd(const fmha_causal_params_t* p) { return whole(p) && p->heads == p->kv_heads && (int64_t)p->batch * p->heads >= 512; }
 
+// `needed`: by this call.  There is one to be used again only where the forward makes one.
 int launch_list(const fmha_causal_params_t* p, const fmha::CausalArgs& a, bool needed, hipStream_t st) {
-  if (!needed || p->batch <= fmha::kCausalSelf || (p->flags & FMHA_FLAG_REUSE_SCHEDULE)) return FMHA_OK;
+  if (!needed || p->batch <= fmha::kCausalSelf || ((p->flags & FMHA_FLAG_REUSE_SCHEDULE) && !whole(p))) return FMHA_OK;
   const Workspace w = carve(p->batch, p->total_tokens, p->heads, p->kv_heads, p->head_dim);
   char* base = static_cast<char*>(p->workspace);
   fmha::causal_list_kernel<<<2, fmha::kCausalListThreads, 0, st>>>(a, reinterpret_cast<int32_t*>(base),
@@ -165,9 +169,9 @@ int launch_list(const fmha_causal_params_t* p, const fmha::CausalArgs& a, bool n
   return FMHA_OK;
 }
 
-// Workgroups for a pass over the tiles of `heads` heads in up to `parts` parts each, and the order in which it takes them.
-unsigned plan(const fmha_causal_params_t* p, int heads, int parts, fmha::CausalArgs* a) {
-  const unsigned items = grid_of(p, heads);
+// Items of a pass over the tiles of `heads` heads, and the order in which it takes them.
+int64_t plan(const fmha_causal_params_t* p, int heads, fmha::CausalArgs* a) {
+  const int64_t items = items_of(p, heads);
   a->by_cost = items <= kByCost;
   if (p->batch > fmha::kCausalSelf) {
     const Workspace w = carve(p->batch, p->total_tokens, p->heads, p->kv_heads, p->head_dim);
@@ -175,14 +179,14 @@ unsigned plan(const fmha_causal_params_t* p, int heads, int parts, fmha::CausalA
     a->count = reinterpret_cast<int32_t*>(base);
     a->list = reinterpret_cast<fmha::TileItem*>(base + (a->by_cost ? w.by_cost : w.by_sequence));
   }
-  return items * (unsigned)parts;
+  return items;
 }
 
 template <typename T, int D>
 int launch_fwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st) {
   a.whole = whole(p);
-  const unsigned grid = a.whole ? (unsigned)(p->batch * a.heads) : plan(p, a.heads, 1, &a);
-  fmha::causal_fwd_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
+  const int64_t items = a.whole ? (int64_t)p->batch * a.heads : plan(p, a.heads, &a);
+  fmha::causal_fwd_kernel<T, D><<<grid(items), fmha::kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal forward launch failed: %s", hipGetErrorString(e));
   return FMHA_OK;
@@ -191,21 +195,21 @@ int launch_fwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st
 template <typename T, int D>
 int launch_bwd(const fmha_causal_params_t* p, fmha::CausalArgs a, hipStream_t st) {
   if (whole_bwd(p)) {
-    fmha::causal_bwd_whole_kernel<T, D><<<(unsigned)(p->batch * a.kv_heads), fmha::kThreads, 0, st>>>(a);
+    fmha::causal_bwd_whole_kernel<T, D><<<grid((int64_t)p->batch * a.kv_heads), fmha::kThreads, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal backward launch failed: %s", hipGetErrorString(e));
     return FMHA_OK;
   }
-  unsigned grid = plan(p, a.heads, 1, &a);
-  fmha::causal_dq_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
+  int64_t items = plan(p, a.heads, &a);
+  fmha::causal_dq_kernel<T, D><<<grid(items), fmha::kThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal dQ launch failed: %s", hipGetErrorString(e));
-  grid = plan(p, a.kv_heads, a.parts, &a);
-  fmha::causal_dkv_kernel<T, D><<<grid, fmha::kThreads, 0, st>>>(a);
+  items = plan(p, a.kv_heads, &a);
+  fmha::causal_dkv_kernel<T, D><<<grid(items * a.parts), fmha::kThreads, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal dK/dV launch failed: %s", hipGetErrorString(e));
   if (a.parts == 1) return FMHA_OK;
-  fmha::causal_dkv_join_kernel<T, D><<<grid / a.parts, fmha::kThreads, 0, st>>>(a);
+  fmha::causal_dkv_join_kernel<T, D><<<grid(items), fmha::kThreads, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "causal dK/dV join launch failed: %s", hipGetErrorString(e));
   return FMHA_OK;

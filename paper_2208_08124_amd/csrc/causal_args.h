@@ -149,17 +149,19 @@ __device__ __forceinline__ TileItem causal_find(const CausalArgs& a, int rank) {
   return ti;
 }
 
-__device__ __forceinline__ TileItem causal_tile(const CausalArgs& a, int rank) {
-  if (!a.list) return causal_find(a, rank);
-  if (rank >= *(ConstInt)(uintptr_t)a.count) return TileItem{0, 0, 0, 0};
-  ConstInt p = (ConstInt)(uintptr_t)(a.list + rank);
-  return TileItem{p[0], p[1], 0, p[3]};
-}
-
 // Number of tiles.
 __device__ __forceinline__ int causal_count(const CausalArgs& a) {
-  if (a.list) return *(ConstInt)(uintptr_t)a.count;
+  if (a.list) return min(*(ConstInt)(uintptr_t)a.count, a.total / kTileRows + a.batch);
   return wave_sum(CausalLane(a).from(0));
+}
+
+// (Whatever the workspace holds, where a call says that its list is there: rows inside the tensors.)
+__device__ __forceinline__ TileItem causal_tile(const CausalArgs& a, int rank) {
+  if (!a.list) return causal_find(a, rank);
+  if (rank >= causal_count(a)) return TileItem{0, 0, 0, 0};
+  ConstInt p = (ConstInt)(uintptr_t)(a.list + rank);
+  const int r0 = min(max(p[0], 0), a.total), len = min(max(p[1], 0), a.total - r0);
+  return TileItem{r0, len, 0, min(max(p[3], 0), max(len - 1, 0)) / kTileRows * kTileRows};
 }
 
 // The same for more sequences, as lists: count <- number of tiles, by_sequence and by_cost <- the tiles.  A workgroup for each list.

@@ -264,6 +264,34 @@ def test_reruns_reuse_of_the_list_and_refusal():
     assert e.value.code == fmha.FMHA_ERR_WORKSPACE
 
 
+@pytest.mark.parametrize("heads,kv_heads,d", [(6, 2, 64), (4, 4, 64), (2, 1, 128)])
+def test_reuse_after_a_forward_that_needs_no_list(heads, kv_heads, d):
+    """More than 256 sequences of one tile each: the forward makes no list, so the backward has none to use again."""
+    b = Batch([1 + (37 * i) % 100 for i in range(300)], heads, kv_heads, d, "bf16", seed=5)
+    b.ws.fill_(0x7F)
+    b.fwd()
+    b.bwd(reuse_schedule=True)
+    again = b.outputs()
+    b.bwd()
+    assert all(torch.equal(x, y) for x, y in zip(again, b.outputs()))
+    check(b, sequences=range(0, 300, 23))
+
+
+@pytest.mark.parametrize("longest", [0, 1])
+def test_more_items_than_a_launch_has_workgroups(longest):
+    """2^18 sequences of one token, 64 heads: a token's output is its value, its dV the sum of dO over the group."""
+    b = Batch([1] * (1 << 18), 64, 8, 64, "bf16", seed=6)
+    b.fwd(longest=longest)
+    b.bwd(longest=longest)
+    assert torch.equal(b.o.view(-1, 8, 8, 64), b.v[:, :, None].expand(-1, 8, 8, 64))
+    want = b.do.view(-1, 8, 8, 64).float().sum(2)
+    # eight summands in fp32: seven sums, each off by at most 2^-24 of the summands' magnitudes; then one rounding, on both sides
+    assert ((b.dv.float() - want).abs() <= 2.0 ** -8 * want.abs() + 14 * 2.0 ** -24 * b.do.view(-1, 8, 8, 64).float().abs().sum(2)).all()
+    # (dS = P (dP - D), D being rowsum(P o dP) for such rows: 64 products on both sides)
+    tol = b.scale * 130 * 2.0 ** -24 * (b.do.float().abs() * b.o.float().abs()).sum(2, keepdim=True)
+    assert (b.dq.float().abs() <= tol * b.k.float().abs().repeat_interleave(8, 1) + 1e-30).all()
+
+
 def test_gradients_against_differences():
     """Central differences of the float64 forward along random directions, h^2 = 1e-8 of third derivatives of order one; the
     kernel's gradients carry their 16-bit roundings, 2^-9 of the sum of magnitudes."""
