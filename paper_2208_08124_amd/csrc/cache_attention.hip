@@ -48,8 +48,9 @@ size_t bytes_of(const Split& s, int32_t batch, int32_t heads, int32_t head_dim) 
 template <typename T, int D>
 int launch(const fmha::CacheArgs& a, hipStream_t st) {
   const int64_t grid = (int64_t)a.splits * a.batch * a.kv_heads * a.tiles;
-  if (grid > 0x7fffffff || (int64_t)a.batch * a.heads > 0x7fffffff)
-    return fail(FMHA_ERR_INVALID_ARG, "batch=%d, heads=%d: more than 2^31 workgroups", a.batch, a.heads);
+  // (a launch holds less than 2^32 threads)
+  if (grid >= (int64_t)1 << 23 || (int64_t)a.batch * a.heads >= (int64_t)1 << 24)
+    return fail(FMHA_ERR_INVALID_ARG, "batch=%d, heads=%d: more workgroups than a launch holds", a.batch, a.heads);
   if (a.waves == 8)
     fmha::cache_attention_kernel<T, D, 8><<<(unsigned)grid, 512, 0, st>>>(a);
   else

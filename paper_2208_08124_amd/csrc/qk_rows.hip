@@ -76,7 +76,7 @@ int64_t cut(fmha::QkRows* a, int64_t enough) {
 
 constexpr int kWaves = fmha::kQkThreads / 64, kFwdWaves = 256 * 4 * 8, kBwdGroups = 256 * 3;  // (what the chip holds at a time)
 
-unsigned fwd_grid(fmha::QkRows* a) { return (unsigned)((cut(a, kFwdWaves) + kWaves - 1) / kWaves); }
+int64_t fwd_grid(fmha::QkRows* a) { return (cut(a, kFwdWaves) + kWaves - 1) / kWaves; }
 
 // Workgroups of the backward, which go over the items in strides: as many as run at a time.  32 265 rows, 32 + 8 heads of 128:
 // 206 us, 233 with 1024 workgroups, the last 256 of which run by themselves.
@@ -86,18 +86,20 @@ int bwd_grid(fmha::QkRows* a) {
 }
 
 template <bool CACHE>
-int launch_rows(const fmha::QkRows& a, unsigned grid, int dtype, int layout, hipStream_t st) {
+int launch_rows(const fmha::QkRows& a, int64_t grid, int dtype, int layout, hipStream_t st) {
+  if (grid >= (int64_t)1 << 24)  // (a launch holds less than 2^32 threads)
+    return fail(FMHA_ERR_INVALID_ARG, "rows=%d of %d heads: more workgroups than a launch holds", a.rows, a.nq + a.nk + a.nv);
   const bool inter = layout == FMHA_ROPE_INTERLEAVED && a.rot;
   if (dtype == FMHA_F16) {
     if (inter)
-      fmha::qk_rows_kernel<_Float16, true, CACHE><<<grid, fmha::kQkThreads, 0, st>>>(a);
+      fmha::qk_rows_kernel<_Float16, true, CACHE><<<(unsigned)grid, fmha::kQkThreads, 0, st>>>(a);
     else
-      fmha::qk_rows_kernel<_Float16, false, CACHE><<<grid, fmha::kQkThreads, 0, st>>>(a);
+      fmha::qk_rows_kernel<_Float16, false, CACHE><<<(unsigned)grid, fmha::kQkThreads, 0, st>>>(a);
   } else {
     if (inter)
-      fmha::qk_rows_kernel<__bf16, true, CACHE><<<grid, fmha::kQkThreads, 0, st>>>(a);
+      fmha::qk_rows_kernel<__bf16, true, CACHE><<<(unsigned)grid, fmha::kQkThreads, 0, st>>>(a);
     else
-      fmha::qk_rows_kernel<__bf16, false, CACHE><<<grid, fmha::kQkThreads, 0, st>>>(a);
+      fmha::qk_rows_kernel<__bf16, false, CACHE><<<(unsigned)grid, fmha::kQkThreads, 0, st>>>(a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(FMHA_ERR_HIP, "norm and rotation launch failed: %s", hipGetErrorString(e));
@@ -180,7 +182,7 @@ int fmha_qk_norm_rope_fwd(const fmha_qk_params_t* p, const void* q, const void* 
   a.k = static_cast<const uint16_t*>(k);
   a.qo = static_cast<uint16_t*>(q_out);
   a.ko = static_cast<uint16_t*>(k_out);
-  const unsigned grid = fwd_grid(&a);
+  const int64_t grid = fwd_grid(&a);
   return launch_rows<false>(a, grid, p->dtype, p->rope.layout, static_cast<hipStream_t>(stream));
 }
 
@@ -291,7 +293,7 @@ int fmha_cache_append(const fmha_cache_t* c, const fmha_append_params_t* p, cons
   a.page_shift = fmha_host::page_shift(c);
   a.num_pages = c->num_pages;
   a.max_pages = c->max_pages;
-  const unsigned grid = fwd_grid(&a);
+  const int64_t grid = fwd_grid(&a);
   return launch_rows<true>(a, grid, c->dtype, p->rope.layout, static_cast<hipStream_t>(stream));
 }
 

@@ -173,9 +173,9 @@ template <bool CACHE>
 __device__ __forceinline__ int qk_position(const QkRows& a, int tok0, int tpw, int mine, int present, int& seq) {
   int pos = 0;
   seq = 0;
-  if (!CACHE && a.positions) return tok0 + mine < present ? a.positions[tok0 + mine] : 0;
+  if (!CACHE && a.positions) return mine < present - tok0 ? a.positions[tok0 + mine] : 0;
   if (!a.cu) {
-    if (CACHE && tok0 + mine < present) {
+    if (CACHE && mine < present - tok0) {
       seq = tok0 + mine;
       pos = a.seqlens[seq] - 1;
     }
@@ -188,9 +188,8 @@ __device__ __forceinline__ int qk_position(const QkRows& a, int tok0, int tpw, i
     end = a.cu[lane + 1];
     if (CACHE) held = a.seqlens[lane];
   }
-  for (int i = 0; i < tpw; i++) {
+  for (int i = 0; i < min(tpw, present - tok0); i++) {
     const int t = tok0 + i;
-    if (t >= present) break;
     int s, at;
     if (a.batch <= 64) {
       s = min((int)__popcll(__ballot(end <= t)), a.batch - 1);
@@ -220,7 +219,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_rows_kernel(const QkRows a) {
   const int tok0 = __builtin_amdgcn_readfirstlane((int)(group * tpw));
   const int part = (int)(wave - group * a.parts);
   const int c = lane % a.lp2, slot = lane / a.lp2;
-  const int mine = slot / a.gs, tok = tok0 + mine;
+  const int mine = slot / a.gs, tok = tok0 + min(mine, present - tok0);  // (= present: no row)
   const bool on = c < a.lph;  // not one of the lanes that a head is padded with
   const QkPieces pc = QkPieces::of<INTER>(c, a.lph, a.rot);
   const int heads = a.nq + a.nk + a.nv;
@@ -302,7 +301,7 @@ __global__ __launch_bounds__(kQkThreads, 3) void qk_rows_bwd_kernel(const QkRows
   const bool on = c < a.lph;
   const QkPieces pc = QkPieces::of<INTER>(c, a.lph, a.rot);
   const int heads = a.nq + a.nk;
-  const int items = (present + tpw - 1) / tpw * a.parts;
+  const int items = present > 0 ? ((present - 1) / tpw + 1) * a.parts : 0;
   for (int i = threadIdx.x; i < a.dim; i += kQkThreads) {
     sums[0][0][i] = a.gamma_q ? a.gamma_q[i] : 1.f;
     sums[0][1][i] = a.gamma_k ? a.gamma_k[i] : 1.f;
@@ -329,7 +328,7 @@ __global__ __launch_bounds__(kQkThreads, 3) void qk_rows_bwd_kernel(const QkRows
   float sum_q[16] = {}, sum_k[16] = {};
   for (int item = blockIdx.x * (kQkThreads / 64) + w; item < items; item += gridDim.x * (kQkThreads / 64)) {
     const int group = item / a.parts, part = item - group * a.parts;
-    const int tok0 = __builtin_amdgcn_readfirstlane(group * tpw), tok = tok0 + mine;
+    const int tok0 = __builtin_amdgcn_readfirstlane(group * tpw), tok = tok0 + min(mine, present - tok0);
     const int first = part * a.iters * a.gs + slot % a.gs, last = min(heads, first + a.iters * a.gs);
     Raw cur;
     fetch(cur, tok, first, last);

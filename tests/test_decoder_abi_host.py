@@ -174,6 +174,20 @@ def test_cache_attention_refusals():
     assert f(2, 4, 2, 64, 100) == 0 and f(2, 4, 2, 64, 100000) > 0  # one workgroup each, and several
 
 
+def test_sizes_that_no_launch_holds():
+    """A launch has less than 2^32 threads."""
+    from paper_2208_08124_amd import fmha
+    lib, INV = fmha.lib(), fmha.FMHA_ERR_INVALID_ARG
+    p = qk(fmha, rows=1 << 28, head_dim=256, q_heads=64, k_heads=64)
+    assert lib.fmha_qk_norm_rope_fwd(ctypes.byref(p), P, P, P, P, None) == INV and "workgroups" in fmha.last_error(), fmha.last_error()
+    c, p = cache(fmha, batch=1 << 28, kv_heads=64, head_dim=256), append(fmha, rows=1 << 28, q_heads=64)
+    assert lib.fmha_cache_append(ctypes.byref(c), ctypes.byref(p), *[P] * 6, None) == INV and "workgroups" in fmha.last_error(), fmha.last_error()
+    for batch, heads in ((1 << 23, 1), (1 << 20, 16)):
+        c = cache(fmha, batch=batch, kv_heads=1)
+        assert lib.fmha_cache_attention(ctypes.byref(c), heads, 4096, 0.125, P, 0, P, P, P, 0, P, P, 1 << 50, None) == INV
+        assert "workgroups" in fmha.last_error(), fmha.last_error()
+
+
 def causal(fmha, **over):
     p = fmha.CausalParams(batch=2, total_tokens=16, heads=4, kv_heads=2, head_dim=64, max_seqlen=8, dtype=0, scale=0.125, cu_seqlens=P,
                           workspace=P, workspace_bytes=1 << 20)
