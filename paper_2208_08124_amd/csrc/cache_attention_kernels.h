@@ -228,7 +228,7 @@ __global__ __launch_bounds__(64 * W, D == 64 ? 3 : 2) void cache_attention_kerne
     }
     const float inv = total > 0.f || total != total ? 1.f / total : 0.f;  // (a NaN among the scores stays one)
     r *= inv;
-    const float lse2 = top == -INFINITY ? top : top + __log2f(total);
+    const float lse2 = top + __log2f(total);  // (no key: -inf, twice)
     if (a.splits == 1) {
       const u32x2 w2 = {Op<T>::pack2(r[0], r[1]), Op<T>::pack2(r[2], r[3])};
       *reinterpret_cast<u32x2*>(a.o + b * a.o_stride + (int64_t)(h0 + h) * D + x) = w2;
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_join_kernel(const CacheAr
   }
   const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
   *reinterpret_cast<uint32_t*>(a.o + b * a.o_stride + (int64_t)h * D + 2 * tid) = Op<T>::pack2(r0 * inv, r1 * inv);
-  if (tid == 0) a.lse[at] = top == -INFINITY ? top : (top + __log2f(total)) * kLn2;
+  if (tid == 0) a.lse[at] = (top + __log2f(total)) * kLn2;
 }
 
 }  // namespace fmha

@@ -130,6 +130,19 @@ def test_scores_that_climb():
     check(s, *call(s, 0.125, 2000), 0.125)
 
 
+@pytest.mark.parametrize("n", [1, 200, 3000])
+def test_nan_queries(n):
+    """A NaN in one head's query: that head's output and log-sum-exp are NaN, whole or split, the others' are not."""
+    s = make_cache([n, 40], 4, 2, 64, 16, "bf16")
+    s["q"][0, 1, 5] = float("nan")
+    o, lse = call(s, 0.125, n)
+    assert torch.isnan(o[0, 1]).all() and torch.isnan(lse[0, 1])
+    s["q"][0, 1] = 0
+    clean_o, clean_lse = call(s, 0.125, n)
+    o[0, 1], lse[0, 1] = clean_o[0, 1], clean_lse[0, 1]
+    assert torch.equal(o, clean_o) and torch.equal(lse, clean_lse)
+
+
 def test_pages_that_are_none():
     """Numbers outside the cache name no page, tokens behind the table do not exist, lengths below zero are none."""
     page, lens = 16, [100, 64, 40, 30]
