@@ -21,7 +21,8 @@
  * them on the unpadded storage, each documented where it is declared: dropout on the
  * attention probabilities, the padded <-> unpadded conversions (Sections IV-A-1, IV-B-2),
  * the fused Dropout + Add + LayerNorm (Section IV-C-1) and the embedding backward
- * (Section IV-C-3).
+ * (Section IV-C-3).  Beyond the paper it has the attention block of a decoder on the same
+ * storage: causal attention with grouped heads, norm and rotation, a paged cache (at the end).
  *
  * Conventions
  *   - Every pointer named "device" is GPU memory owned by the caller; the
