@@ -149,16 +149,20 @@ __device__ __forceinline__ TileItem causal_find(const CausalArgs& a, int rank) {
   return ti;
 }
 
+// Tiles that any lengths can have, which the workspace is sized by.  (Prefix sums that fall and rise again would have more: the
+// rest is left.)
+__device__ __forceinline__ int causal_capacity(const CausalArgs& a) { return a.total / kTileRows + a.batch; }
+
 // Number of tiles.
 __device__ __forceinline__ int causal_count(const CausalArgs& a) {
-  if (a.list) return min(*(ConstInt)(uintptr_t)a.count, a.total / kTileRows + a.batch);
-  return wave_sum(CausalLane(a).from(0));
+  return min(a.list ? *(ConstInt)(uintptr_t)a.count : wave_sum(CausalLane(a).from(0)), causal_capacity(a));
 }
 
-// (Whatever the workspace holds, where a call says that its list is there: rows inside the tensors.)
 __device__ __forceinline__ TileItem causal_tile(const CausalArgs& a, int rank) {
+  if (rank >= causal_capacity(a)) return TileItem{0, 0, 0, 0};
   if (!a.list) return causal_find(a, rank);
-  if (rank >= causal_count(a)) return TileItem{0, 0, 0, 0};
+  // (rows inside the tensors, whatever the workspace holds where a call says that its list is there)
+  if (rank >= *(ConstInt)(uintptr_t)a.count) return TileItem{0, 0, 0, 0};
   ConstInt p = (ConstInt)(uintptr_t)(a.list + rank);
   const int r0 = min(max(p[0], 0), a.total), len = min(max(p[1], 0), a.total - r0);
   return TileItem{r0, len, 0, min(max(p[3], 0), max(len - 1, 0)) / kTileRows * kTileRows};

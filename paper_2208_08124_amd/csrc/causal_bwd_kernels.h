@@ -340,7 +340,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void causal_dkv_kernel(const CausalArgs a) {
   __shared__ __align__(1024) CausalDkvLds<D> lds;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int round = a.parts > 1 ? causal_count(a) * a.kv_heads : 0x7fffffff;  // the items' first parts, then their second ones, ..
+  const int round = a.parts > 1 ? max(causal_count(a), 1) * a.kv_heads : 0x7fffffff;  // the items' first parts, then their second ones, ..
   for (int item = blockIdx.x;; item += gridDim.x) {
     const int part = item / round, index = item - part * round;
     if (part >= a.parts) return;

@@ -247,6 +247,30 @@ def test_prefix_sums_that_disagree_with_the_sizes():
         assert torch.equal(b.o[:40], want[:40])
 
 
+@pytest.mark.parametrize("batch", [64, 400])
+def test_prefix_sums_that_rise_again_and_again(batch):
+    """More tiles than any well-formed prefix sums have: what stands behind the workspace and the rows is left alone."""
+    b = Batch([1500], 8, 1, 128, "bf16", behind=100)
+    b.cu = torch.tensor([0, 1500] * (batch // 2) + [0], dtype=torch.int32, device="cuda")
+    n = fmha.fmha_causal_workspace_size(batch, b.t, 8, 1, 128, True)
+    whole = torch.full((n + (1 << 20),), 7, dtype=torch.uint8, device="cuda")
+    b.ws = whole[:n]
+    b.fwd()
+    b.bwd()
+    torch.cuda.synchronize()
+    assert (whole[n:] == 7).all()
+    assert all(torch.isnan(x[1500:]).all() for x in (b.o, b.dq, b.dk, b.dv)) and torch.isnan(b.lse[:, 1500:]).all()
+
+
+@pytest.mark.parametrize("batch", [1, 5, 300])
+def test_nothing_but_empty_sequences(batch):
+    b = Batch([0] * batch, 8, 1, 128, "f16", behind=2000)
+    for longest in (0, 2000):
+        b.fwd(longest=longest)
+        b.bwd(longest=longest)
+    assert all(torch.isnan(x).all() for x in b.outputs())
+
+
 def test_reruns_reuse_of_the_list_and_refusal():
     b = Batch([129, 7, 0, 64, 1] * 60, 4, 2, 64, "bf16")
     b.fwd()
