@@ -496,7 +496,7 @@ int fmha_cache_attention(const fmha_cache_t* c, int32_t heads, int32_t max_seqle
  *   max_seqlen being the same: they decide in how many parts a long sum is taken, which may move a result by a rounding).
  * Rows at and beyond cu_seqlens[batch] are neither read nor written.  The backward needs the forward's o and lse, and a
  * workspace sized with need_bwd (few long sequences: up to 512 MiB more, for sums taken in parts).  Calls that may overlap in
- * time need workspaces of their own.
+ * time need workspaces of their own.  Outputs must not overlap inputs or each other.
  * An infinity or NaN in a sequence's k, v, q or d_o may reach any of its rows (a masked probability is 0, and 0 * inf is NaN), but no
  * other sequence's. */
 typedef struct fmha_causal_params {
