@@ -272,6 +272,7 @@ def _params(q, cu_seqlens, max_seqlen, scale, workspace, seqused, cu_seqlens_hos
 # The current stream's handle, without the Stream object around it: 0.3 us a call in place of 2.8, of the 9 that
 # the smallest calls take.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (0.1 us in place of 0.2)
 
 
 def _stream():
@@ -512,7 +513,7 @@ def fmha_rope_frequencies(rotary_dim, base=10000.0, scaling="plain", factor=1.0,
 
 def _here(*tensors):
     """The current stream's handle; refuses tensors that are not on the current device, whose stream that is."""
-    dev = torch.cuda.current_device()
+    dev = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise FmhaError(FMHA_ERR_INVALID_ARG, f"a tensor is on {t.device}, the current device is cuda:{dev}")
@@ -647,24 +648,32 @@ def fmha_cache_append(k, v, k_cache, v_cache, block_table, seqlens, *, cu_seqlen
     k and written to q_out (which may be q)."""
     c = _cache(k_cache, v_cache, block_table, seqlens)
     p = AppendParams()
-    p.rows = k.shape[0]
-    assert k.shape[1:] == (c.kv_heads, c.head_dim) and k.dtype == k_cache.dtype
-    _same_kind(k, v)
-    assert cu_seqlens is None or cu_seqlens.numel() == c.batch + 1
-    p.eps = float(eps)
+    shape, dtype, dim = k.shape, k.dtype, k_cache.shape[3]
+    assert len(shape) == 3 and shape[1] == k_cache.shape[1] and shape[2] == dim and dtype == k_cache.dtype
+    assert v.shape == shape and v.dtype == dtype
+    p.rows, p.eps = shape[0], eps
     p.k_stride, p.v_stride = _tok_stride(k), _tok_stride(v)
+    q_ptr = q_out_ptr = None
     if q is not None:
-        assert q.shape[0] == k.shape[0] and q.shape[2] == k.shape[2] and q.dtype == k.dtype
-        _same_kind(q, q_out)
-        p.q_heads = q.shape[1]
-        p.q_stride, p.q_out_stride = _tok_stride(q), _tok_stride(q_out)
-    p.gamma_q, p.gamma_k = _gamma_ptr(gamma_q, c.head_dim), _gamma_ptr(gamma_k, c.head_dim)
-    p.cu_seqlens = _i32_ptr(cu_seqlens)
-    p.rope = _rope(rope)
+        q_shape = q.shape
+        assert q_shape[0] == shape[0] and q_shape[2] == dim and q.dtype == dtype
+        p.q_heads, p.q_stride, q_ptr = q_shape[1], _tok_stride(q), q.data_ptr()
+        if q_out is not None:
+            assert q_out.shape == q_shape and q_out.dtype == dtype
+            p.q_out_stride, q_out_ptr = _tok_stride(q_out), q_out.data_ptr()
+    if gamma_q is not None:
+        p.gamma_q = _gamma_ptr(gamma_q, dim)
+    if gamma_k is not None:
+        p.gamma_k = _gamma_ptr(gamma_k, dim)
+    if cu_seqlens is not None:
+        assert cu_seqlens.numel() == seqlens.numel() + 1
+        p.cu_seqlens = _i32_ptr(cu_seqlens)
+    if rope is not None:
+        p.rope = _rope(rope)
     stream = _here(k, v, k_cache, v_cache, block_table, seqlens, cu_seqlens, q, q_out, gamma_q, gamma_k,
                    None if rope is None else rope[0])
-    _check(lib().fmha_cache_append(ctypes.byref(c), ctypes.byref(p), _opt_ptr(q), k.data_ptr(), v.data_ptr(),
-                                   _opt_ptr(q_out), k_cache.data_ptr(), v_cache.data_ptr(), stream))
+    _check(lib().fmha_cache_append(ctypes.byref(c), ctypes.byref(p), q_ptr, k.data_ptr(), v.data_ptr(), q_out_ptr,
+                                   k_cache.data_ptr(), v_cache.data_ptr(), stream))
 
 
 def fmha_cache_attention_workspace_size(batch: int, heads: int, kv_heads: int, head_dim: int, max_seqlen: int) -> int:
